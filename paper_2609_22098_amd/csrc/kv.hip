@@ -1,0 +1,199 @@
+// C ABI of the target's 4-bit key-value cache (treespark_kv.h): argument checks and launches.
+#include <cmath>
+
+#include "host_api.hpp"
+#include "kv_launch.hpp"
+
+namespace ts {
+namespace {
+
+constexpr int kMaxRequests = 65536;
+
+bool page_size_ok(int32_t p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
+bool head_dim_ok(int32_t d) { return d == 64 || d == 128 || d == 256; }
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int32_t check_cache(const ts_kv_cache* c) {
+  if (!c) return fail(TS_EINVAL, "cache is NULL");
+  if (!c->pages) return fail(TS_EINVAL, "cache pages pointer is NULL");
+  if (c->layers < 1 || c->num_pages < 1 || c->heads < 1)
+    return fail(TS_EINVAL, "cache sizes must be positive (layers=%d num_pages=%d heads=%d)", c->layers, c->num_pages, c->heads);
+  if (!page_size_ok(c->page_size)) return fail(TS_EUNSUPPORTED, "page_size=%d is not 16, 32, 64, 128 or 256", c->page_size);
+  if (!head_dim_ok(c->head_dim)) return fail(TS_EUNSUPPORTED, "head_dim=%d is not 64, 128 or 256", c->head_dim);
+  if ((int64_t)c->num_pages * c->page_size >= (int64_t)1 << 31)
+    return fail(TS_EUNSUPPORTED, "num_pages * page_size = %lld reaches 2^31", (long long)c->num_pages * c->page_size);
+  if (c->layers > 65535 || c->heads > 65536) return fail(TS_EUNSUPPORTED, "layers=%d or heads=%d out of range", c->layers, c->heads);
+  if (!aligned16(c->pages) || c->page_stride % 16 || c->layer_stride % 16)
+    return fail(TS_EINVAL, "cache pages and strides must be multiples of 16 bytes");
+  const int64_t block = (int64_t)c->heads * (int64_t)ts_kv_block_bytes(c->page_size, c->head_dim);
+  if (c->page_stride < block) return fail(TS_EINVAL, "page_stride %lld < %lld bytes of a page", (long long)c->page_stride, (long long)block);
+  if (c->layers > 1 && c->layer_stride < block)
+    return fail(TS_EINVAL, "layer_stride %lld < %lld bytes of a page", (long long)c->layer_stride, (long long)block);
+  return TS_OK;
+}
+
+int32_t check_layer(const ts_kv_cache* c, int32_t layer, int32_t layers) {
+  if (layer < 0 || layers < 1 || layer > c->layers - layers)
+    return fail(TS_EINVAL, "layers [%d, %lld) outside [0, %d)", layer, (long long)layer + layers, c->layers);
+  return TS_OK;
+}
+
+int32_t check_dtype(int32_t dtype) {
+  if (dtype != TS_F32 && dtype != TS_BF16) return fail(TS_EINVAL, "unknown dtype %d", dtype);
+  return TS_OK;
+}
+
+int32_t check_requests(int32_t R, int32_t max_blocks, int32_t page_size) {
+  if (R < 0) return fail(TS_EINVAL, "R=%d is negative", R);
+  if (R > kMaxRequests) return fail(TS_EUNSUPPORTED, "R=%d exceeds %d", R, kMaxRequests);
+  if (max_blocks < 1) return fail(TS_EINVAL, "max_blocks=%d", max_blocks);
+  if ((int64_t)max_blocks * page_size > (int64_t)1 << 30)
+    return fail(TS_EUNSUPPORTED, "max_blocks * page_size = %lld exceeds 2^30", (long long)max_blocks * page_size);
+  if ((int64_t)R * max_blocks >= (int64_t)1 << 31)
+    return fail(TS_EUNSUPPORTED, "R * max_blocks = %lld reaches 2^31", (long long)R * max_blocks);
+  return TS_OK;
+}
+
+int log2i(int x) { return __builtin_ctz((unsigned)x); }
+
+KvView view(const ts_kv_cache* c, int32_t layer) {
+  return {static_cast<char*>(c->pages) + (int64_t)layer * c->layer_stride, c->layer_stride, c->page_stride,
+          c->num_pages, log2i(c->page_size), c->heads};
+}
+
+int64_t elem_size(int32_t dtype) { return dtype == TS_BF16 ? 2 : 4; }
+
+}  // namespace
+}  // namespace ts
+
+using namespace ts;
+
+#define TS_CHECK(call)                    \
+  do {                                    \
+    if (int32_t rc_ = (call)) return rc_; \
+  } while (0)
+
+extern "C" {
+
+size_t ts_kv_block_bytes(int32_t page_size, int32_t head_dim) {
+  if (!page_size_ok(page_size) || !head_dim_ok(head_dim)) return 0;
+  return (size_t)page_size * head_dim * 17 / 16;
+}
+
+int32_t ts_kv_plan(const int32_t* len, const int32_t* n, int32_t R, int32_t cap, int32_t page_size,
+                   int32_t num_pages, int32_t max_blocks, int32_t* free_pages, int32_t* free_count,
+                   int32_t* held, int32_t* table, int32_t* slot, int32_t* granted, void* stream) {
+  clear_error();
+  if (!page_size_ok(page_size)) return fail(TS_EUNSUPPORTED, "page_size=%d is not 16, 32, 64, 128 or 256", page_size);
+  TS_CHECK(check_requests(R, max_blocks, page_size));
+  if (cap < 1 || cap > TS_KV_MAX_CAP) return fail(TS_EINVAL, "cap=%d outside [1, %d]", cap, TS_KV_MAX_CAP);
+  if ((int64_t)R * cap >= (int64_t)1 << 31) return fail(TS_EUNSUPPORTED, "R * cap = %lld reaches 2^31", (long long)R * cap);
+  if (num_pages < 1) return fail(TS_EINVAL, "num_pages=%d", num_pages);
+  if ((int64_t)num_pages * page_size >= (int64_t)1 << 31)
+    return fail(TS_EUNSUPPORTED, "num_pages * page_size = %lld reaches 2^31", (long long)num_pages * page_size);
+  if (R == 0) return TS_OK;
+  if (!len || !n || !free_pages || !free_count || !held || !table || !granted)
+    return fail(TS_EINVAL, "a required array is NULL");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const KvPlanParams p = {len, n, R, cap, log2i(page_size), num_pages, max_blocks,
+                          free_pages, free_count, held, table, slot, granted};
+  launch_kv_plan(p, s);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}
+
+int32_t ts_kv_append(const ts_kv_cache* cache, int32_t layer, const void* k, const void* v, int32_t dtype,
+                     int64_t k_stride, int64_t v_stride, const int32_t* slot, int32_t rows, void* stream) {
+  clear_error();
+  TS_CHECK(check_cache(cache));
+  TS_CHECK(check_layer(cache, layer, 1));
+  TS_CHECK(check_dtype(dtype));
+  if (rows < 0) return fail(TS_EINVAL, "rows=%d is negative", rows);
+  if (rows == 0) return TS_OK;
+  if (!k || !v || !slot) return fail(TS_EINVAL, "k, v or slot is NULL");
+  const int64_t width = (int64_t)cache->heads * cache->head_dim, unit = 16 / elem_size(dtype);
+  if (k_stride < width || v_stride < width || k_stride % unit || v_stride % unit)
+    return fail(TS_EINVAL, "strides %lld, %lld: at least %lld elements and whole 16 bytes are needed", (long long)k_stride,
+                (long long)v_stride, (long long)width);
+  if (!aligned16(k) || !aligned16(v)) return fail(TS_EINVAL, "k and v must start at 16-byte aligned addresses");
+  if ((int64_t)rows * width >= (int64_t)1 << 40) return fail(TS_EUNSUPPORTED, "rows=%d", rows);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const KvAppendParams p = {view(cache, layer), k, v, k_stride, v_stride, slot, rows};
+  launch_kv_append(p, cache->head_dim, dtype == TS_BF16, s);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}
+
+int32_t ts_kv_read(const ts_kv_cache* cache, int32_t layer, int32_t layers, const int32_t* slot, int32_t rows,
+                   void* k, void* v, int32_t dtype, void* stream) {
+  clear_error();
+  TS_CHECK(check_cache(cache));
+  TS_CHECK(check_layer(cache, layer, layers));
+  TS_CHECK(check_dtype(dtype));
+  if (rows < 0) return fail(TS_EINVAL, "rows=%d is negative", rows);
+  if (rows == 0 || (!k && !v)) return TS_OK;
+  if (!slot) return fail(TS_EINVAL, "slot is NULL");
+  if (!aligned16(k) || !aligned16(v)) return fail(TS_EINVAL, "k and v must start at 16-byte aligned addresses");
+  if ((int64_t)rows * cache->heads * cache->head_dim >= (int64_t)1 << 40) return fail(TS_EUNSUPPORTED, "rows=%d", rows);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const KvReadParams p = {view(cache, layer), slot, rows, layers, k, v};
+  launch_kv_read(p, cache->head_dim, dtype == TS_BF16, s);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}
+
+size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32_t cap, int32_t q_heads, int32_t dtype) {
+  (void)cache, (void)R, (void)cap, (void)q_heads, (void)dtype;
+  return 0;
+}
+
+int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, int32_t dtype, int64_t q_stride,
+                        int32_t q_heads, const int32_t* len, const int32_t* n, int32_t R, int32_t cap,
+                        const int32_t* table, int32_t max_blocks, const uint32_t* mask, float scale, void* out,
+                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  TS_CHECK(check_cache(cache));
+  TS_CHECK(check_layer(cache, layer, 1));
+  TS_CHECK(check_dtype(dtype));
+  TS_CHECK(check_requests(R, max_blocks, cache->page_size));
+  if (q_heads < 1 || q_heads % cache->heads)
+    return fail(TS_EINVAL, "q_heads=%d is no positive multiple of the cache's %d heads", q_heads, cache->heads);
+  const int32_t most = mask ? TS_MAX_CAP : TS_KV_MAX_CAP;
+  if (cap < 1 || cap > most) return fail(TS_EINVAL, "cap=%d outside [1, %d]", cap, most);
+  if ((int64_t)R * cap * q_heads >= (int64_t)1 << 31)
+    return fail(TS_EUNSUPPORTED, "R * cap * q_heads = %lld reaches 2^31", (long long)R * cap * q_heads);
+  if (!std::isfinite(scale)) return fail(TS_EINVAL, "scale must be finite");
+  if (R == 0) return TS_OK;
+  if (!q || !len || !n || !table || !out) return fail(TS_EINVAL, "a required array is NULL");
+  const int64_t width = (int64_t)q_heads * cache->head_dim;
+  if (q_stride < width || q_stride % (16 / elem_size(dtype)))
+    return fail(TS_EINVAL, "q_stride %lld: at least %lld elements and whole 16 bytes are needed", (long long)q_stride, (long long)width);
+  if (!aligned16(q) || !aligned16(out)) return fail(TS_EINVAL, "q and out must start at 16-byte aligned addresses");
+  const size_t need = ts_kv_attention_workspace_size(cache, R, cap, q_heads, dtype);
+  if (workspace_bytes < need) return fail(TS_ENOSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+  if (need && (!workspace || !aligned16(workspace))) return fail(TS_EINVAL, "workspace must be 16-byte aligned memory");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  KvAttnParams p = {view(cache, layer), q, q_stride, q_heads, q_heads / cache->heads, R, cap, max_blocks,
+                    ts_tree_mask_words(cap), len, n, table, mask, scale * kLog2e, out, lse};
+  launch_kv_attention(p, cache->head_dim, dtype == TS_BF16, s);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}
+
+int32_t ts_kv_accept(const ts_kv_cache* cache, const int32_t* len, const int32_t* n, int32_t R,
+                     const int32_t* table, int32_t max_blocks, const int32_t* path_nodes,
+                     const int32_t* path_len, int32_t* new_len, void* stream) {
+  clear_error();
+  TS_CHECK(check_cache(cache));
+  TS_CHECK(check_requests(R, max_blocks, cache->page_size));
+  if (R == 0) return TS_OK;
+  if (!len || !n || !table || !path_nodes || !path_len || !new_len) return fail(TS_EINVAL, "a required array is NULL");
+  if (new_len == len) return fail(TS_EINVAL, "new_len must not be the array len");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const KvAcceptParams p = {view(cache, 0), cache->layers, len, n, table, path_nodes, path_len, R, max_blocks, new_len};
+  launch_kv_accept(p, cache->head_dim, s);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,201 @@
+// Rows into the 4-bit cache, back out of it, and from place to place
+// (ts_kv_append, ts_kv_read, ts_kv_accept).
+#pragma once
+
+#include "kv_format.hpp"
+
+namespace ts {
+
+constexpr int kRowThreads = 256;
+
+// Eight consecutive elements as fp32.
+__device__ __forceinline__ void load8(const float* x, float (&v)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(x), b = *reinterpret_cast<const f32x4*>(x + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = a[i], v[i + 4] = b[i];
+}
+__device__ __forceinline__ void load8(const __bf16* x, float (&v)[8]) {
+  const u32x4 a = *reinterpret_cast<const u32x4*>(x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(a[i] << 16);
+    v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+  }
+}
+
+// Largest magnitude of a group's 32 elements, its four lanes (a quad) agreeing;
+// the bits of magnitudes order as integers do, NaN and infinity on top.
+__device__ __forceinline__ uint32_t group_max_bits(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  m = max(m, (uint32_t)dpp_i32<0xB1>((int)m));
+  return max(m, (uint32_t)dpp_i32<0x4E>((int)m));
+}
+
+// The scale byte of a group: the least e with m <= 7 * 2^(e - 127).  The
+// mantissa of 7 is 1.75: adding just less than what lies above it carries into
+// the exponent exactly where m is more.  The lower bound keeps 127 - e a normal
+// exponent, the upper one 6 * 2^(e - 127) finite.
+__device__ __forceinline__ int group_scale(uint32_t max_bits) {
+  return min(max((int)((max_bits + 0x1FFFFFu) >> 23) - 2, 2), 252);
+}
+
+// Codes of eight values: v_cvt rounds value / scale to the nearest E2M1, ties
+// to the even code, and saturates at 6.
+__device__ __forceinline__ uint32_t encode8(const float (&v)[8], int e) {
+  const float s = __uint_as_float((uint32_t)e << 23);
+  uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], s, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], s, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], s, 3);
+}
+
+// Eight elements of a key and of the value a thread: D / 8 neighbouring lanes
+// hold a (row, head), four a group.
+template <typename TE, int D>
+__global__ __launch_bounds__(kRowThreads) void kv_append_kernel(KvAppendParams p) {
+  constexpr int kLanes = D / 8;
+  const int64_t item = (int64_t)blockIdx.x * (kRowThreads / kLanes) + threadIdx.x / kLanes;
+  const int at = threadIdx.x % kLanes;
+  const int row = (int)(item / p.c.heads), head = (int)(item % p.c.heads);
+  if (row >= p.rows) return;
+  const int slot = p.slot[row], shift = p.c.page_shift;
+  if (slot < 0 || (slot >> shift) >= p.c.num_pages) return;
+  float k[8], v[8];
+  load8(static_cast<const TE*>(p.k) + (int64_t)row * p.k_stride + head * D + at * 8, k);
+  load8(static_cast<const TE*>(p.v) + (int64_t)row * p.v_stride + head * D + at * 8, v);
+  const uint32_t mk = group_max_bits(k), mv = group_max_bits(v);
+  // a NaN or an infinity anywhere in the head
+  uint32_t worst = max(mk, mv);
+#pragma unroll
+  for (int d = 4; d < kLanes; d <<= 1) worst = max(worst, (uint32_t)__shfl_xor((int)worst, d));
+  const bool bad = worst >= 0x7F800000u;
+  int ek = group_scale(mk), ev = group_scale(mv);
+  const uint32_t ck = bad ? 0u : encode8(k, ek), cv = bad ? 0u : encode8(v, ev);
+  if (bad) ek = 255, ev = 2;
+  const int off = slot & ((1 << shift) - 1);
+  char* b = kv_block<D>(p.c, slot >> shift, head);
+  *reinterpret_cast<uint32_t*>(b + KvBlock<D>::key_codes(off) + at * 4) = ck;
+  *reinterpret_cast<uint32_t*>(b + KvBlock<D>::value_codes(off, shift) + at * 4) = cv;
+  if (at % 4 == 0) {
+    b[KvBlock<D>::key_scales(off, shift) + at / 4] = (char)ek;
+    b[KvBlock<D>::value_scales(off, shift) + at / 4] = (char)ev;
+  }
+}
+
+// Eight elements a thread, key and value.
+template <typename TE, int D>
+__device__ __forceinline__ void store8(TE* out, uint32_t codes, uint32_t scale, bool zero, bool nan) {
+  bf16x2 x[4];
+  fp4_to_bf16x8(zero ? 0u : codes, zero || nan ? 127u : scale, x);
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = nan ? 0x7FC07FC0u : __builtin_bit_cast(uint32_t, x[i]);
+  if constexpr (sizeof(TE) == 2) {
+    *reinterpret_cast<u32x4*>(out) = w;
+  } else {
+    f32x4 a, b;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      a[2 * i] = __uint_as_float(w[i] << 16), a[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      b[2 * i] = __uint_as_float(w[i + 2] << 16), b[2 * i + 1] = __uint_as_float(w[i + 2] & 0xFFFF0000u);
+    }
+    *reinterpret_cast<f32x4*>(out) = a;
+    *reinterpret_cast<f32x4*>(out + 4) = b;
+  }
+}
+
+template <typename TE, int D>
+__global__ __launch_bounds__(kRowThreads) void kv_read_kernel(KvReadParams p) {
+  constexpr int kLanes = D / 8;
+  const int64_t item = (int64_t)blockIdx.x * (kRowThreads / kLanes) + threadIdx.x / kLanes;
+  const int at = threadIdx.x % kLanes, layer = blockIdx.y;
+  const int row = (int)(item / p.c.heads), head = (int)(item % p.c.heads);
+  if (row >= p.rows) return;
+  const int slot = p.slot[row], shift = p.c.page_shift;
+  if (slot < 0 || (slot >> shift) >= p.c.num_pages) return;
+  const int off = slot & ((1 << shift) - 1);
+  const char* b = kv_block<D>(p.c, slot >> shift, head) + layer * p.c.layer_stride;
+  const int64_t to = (((int64_t)layer * p.rows + row) * p.c.heads + head) * D + at * 8;
+  if (p.k) {
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(b + KvBlock<D>::key_codes(off) + at * 4);
+    const uint32_t scale = (uint8_t)b[KvBlock<D>::key_scales(off, shift) + at / 4];
+    store8<TE, D>(static_cast<TE*>(p.k) + to, codes, scale, false, scale == 255);
+  }
+  if (p.v) {
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(b + KvBlock<D>::value_codes(off, shift) + at * 4);
+    const uint32_t scale = (uint8_t)b[KvBlock<D>::value_scales(off, shift) + at / 4];
+    store8<TE, D>(static_cast<TE*>(p.v) + to, codes, scale, scale == 255, false);
+  }
+}
+
+// The accepted rows of a request in one layer: a thread owns a word of the
+// rows of one head, reads it of all accepted rows and then writes it, so that no
+// order among the rows matters (a row's new place may be another's old one).
+// A word of a row: D/8 of key codes, then value codes, then D/128 (at least
+// one half) of each scale; scales are moved in pieces of 2 bytes.
+template <int D>
+__global__ __launch_bounds__(kRowThreads) void kv_accept_kernel(KvAcceptParams p) {
+  constexpr int kCodeWords = D / 8, kScaleHalves = D / 64;
+  constexpr int kPieces = 2 * kCodeWords + 2 * kScaleHalves;
+  __shared__ int src[TS_MAX_D], dst[TS_MAX_D];
+  const int q = blockIdx.x, layer = blockIdx.y, t = threadIdx.x;
+  const int shift = p.c.page_shift, limit = p.max_blocks << shift;
+  const int n = p.n[q], count = min(p.path_len[q], TS_MAX_D);
+  const int len = max(p.len[q], 0);
+  const bool on = n >= 0 && count >= 0;
+  if (t < TS_MAX_D) {
+    int from = -1, to = -1;
+    if (on && t < count && len < limit) {
+      const int32_t* row = p.table + (size_t)q * p.max_blocks;
+      const int node = p.path_nodes[q * TS_MAX_D + t], before = t ? p.path_nodes[q * TS_MAX_D + t - 1] : 0;
+      if (node > before && node <= n && node < limit - len) {
+        const int a = len + node, b = len + 1 + t;  // b <= a: the path's nodes increase from 1 on
+        const int pa = kv_page(row, a >> shift, p.max_blocks, p.c.num_pages);
+        const int pb = b < limit ? kv_page(row, b >> shift, p.max_blocks, p.c.num_pages) : -1;
+        const int mask = (1 << shift) - 1;
+        if (pa >= 0 && pb >= 0) from = (pa << shift) + (a & mask), to = (pb << shift) + (b & mask);
+      }
+    }
+    src[t] = from;
+    dst[t] = to;
+  }
+  __syncthreads();
+  int kept = 0;
+  while (kept < TS_MAX_D && src[kept] >= 0) ++kept;
+  if (layer == 0 && t == 0) p.new_len[q] = on ? p.len[q] < 0 ? 1 + kept : p.len[q] + 1 + kept : p.len[q];
+  const int items = p.c.heads * kPieces;
+  const int64_t lay = (int64_t)layer * p.c.layer_stride;
+  for (int it = t; it < items; it += kRowThreads) {
+    const int head = it / kPieces, piece = it % kPieces;
+    uint32_t w[TS_MAX_D];
+    auto place = [&](int slot) {
+      const int off = slot & ((1 << shift) - 1);
+      char* b = kv_block<D>(p.c, slot >> shift, head) + lay;
+      if (piece < kCodeWords) return b + KvBlock<D>::key_codes(off) + piece * 4;
+      if (piece < 2 * kCodeWords) return b + KvBlock<D>::value_codes(off, shift) + (piece - kCodeWords) * 4;
+      const int s = piece - 2 * kCodeWords;
+      if (s < kScaleHalves) return b + KvBlock<D>::key_scales(off, shift) + s * 2;
+      return b + KvBlock<D>::value_scales(off, shift) + (s - kScaleHalves) * 2;
+    };
+    const bool word = piece < 2 * kCodeWords;
+#pragma unroll
+    for (int j = 0; j < TS_MAX_D; ++j)
+      if (j < kept) {
+        const char* a = place(src[j]);
+        w[j] = word ? *reinterpret_cast<const uint32_t*>(a) : *reinterpret_cast<const uint16_t*>(a);
+      }
+#pragma unroll
+    for (int j = 0; j < TS_MAX_D; ++j)
+      if (j < kept) {
+        char* a = place(dst[j]);
+        if (word)
+          *reinterpret_cast<uint32_t*>(a) = w[j];
+        else
+          *reinterpret_cast<uint16_t*>(a) = (uint16_t)w[j];
+      }
+  }
+}
+
+}  // namespace ts

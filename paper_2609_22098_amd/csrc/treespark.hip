@@ -16,6 +16,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "host_api.hpp"
 #include "launch.hpp"
 #include "verify_fused.hpp"
 
@@ -26,9 +27,8 @@
 static __device__ __align__(256) char scratch[TS_NOALLOC_SCRATCH_BYTES];
 
 namespace ts {
-namespace {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 int32_t fail(int32_t code, const char* fmt, ...) {
   char buf[512];
@@ -40,11 +40,9 @@ int32_t fail(int32_t code, const char* fmt, ...) {
   return code;
 }
 
-#define TS_HIP(call)                                                                     \
-  do {                                                                                   \
-    hipError_t e_ = (call);                                                              \
-    if (e_ != hipSuccess) return fail(TS_EHIP, "%s: %s", #call, hipGetErrorString(e_));  \
-  } while (0)
+void clear_error() { g_last_error.clear(); }
+
+namespace {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
