@@ -61,6 +61,43 @@ KvView view(const ts_kv_cache* c, int32_t layer) {
           c->num_pages, log2i(c->page_size), c->heads};
 }
 
+// What a launch of the attention takes: the row tile, the workgroups, and where
+// their partial results lie in the workspace.
+struct AttnPlan {
+  AttnTile tile;
+  int rows, groups;
+  size_t stats, joins, bytes;  // offsets after the parts, and all
+};
+
+// The smallest tile that holds all rows of a request and kv head, so that its
+// keys and values are read once; the largest where none does.
+AttnPlan attn_plan(const ts_kv_cache* c, int32_t cap, int32_t q_heads, int32_t dtype, int cus) {
+  AttnPlan x;
+  const int64_t rows = (int64_t)cap * (q_heads / c->heads);
+  if (dtype == TS_F32)
+    x.tile = rows <= 16 ? AttnTile::k16 : AttnTile::k64;
+  else
+    x.tile = rows <= 16 ? AttnTile::k16 : rows <= 32 ? AttnTile::k32 : rows <= 64 ? AttnTile::k64 : AttnTile::k128;
+  x.rows = 16 << (int)x.tile;
+  x.groups = cus * 2;
+  const size_t parts = (size_t)x.groups * 2 * x.rows;
+  x.stats = parts * c->head_dim * sizeof(float);
+  x.joins = x.stats + parts * sizeof(AttnStat);
+  x.bytes = (x.joins + x.groups * sizeof(AttnJoin) + 255) & ~(size_t)255;
+  return x;
+}
+
+// Compute units of the current device (256 where there is none to ask).
+int compute_units() {
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+      cus < 1) {
+    (void)hipGetLastError();
+    cus = 256;
+  }
+  return cus;
+}
+
 int64_t elem_size(int32_t dtype) { return dtype == TS_BF16 ? 2 : 4; }
 
 }  // namespace
@@ -143,8 +180,11 @@ int32_t ts_kv_read(const ts_kv_cache* cache, int32_t layer, int32_t layers, cons
 }
 
 size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32_t cap, int32_t q_heads, int32_t dtype) {
-  (void)cache, (void)R, (void)cap, (void)q_heads, (void)dtype;
-  return 0;
+  clear_error();
+  if (check_cache(cache) || check_dtype(dtype) || R < 0 || R > kMaxRequests || cap < 1 || cap > TS_KV_MAX_CAP || q_heads < 1 ||
+      q_heads % cache->heads)
+    return 0;
+  return attn_plan(cache, cap, q_heads, dtype, compute_units()).bytes;
 }
 
 int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, int32_t dtype, int64_t q_stride,
@@ -169,13 +209,19 @@ int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, 
   if (q_stride < width || q_stride % (16 / elem_size(dtype)))
     return fail(TS_EINVAL, "q_stride %lld: at least %lld elements and whole 16 bytes are needed", (long long)q_stride, (long long)width);
   if (!aligned16(q) || !aligned16(out)) return fail(TS_EINVAL, "q and out must start at 16-byte aligned addresses");
-  const size_t need = ts_kv_attention_workspace_size(cache, R, cap, q_heads, dtype);
-  if (workspace_bytes < need) return fail(TS_ENOSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
-  if (need && (!workspace || !aligned16(workspace))) return fail(TS_EINVAL, "workspace must be 16-byte aligned memory");
+  const AttnPlan plan = attn_plan(cache, cap, q_heads, dtype, compute_units());
+  if (workspace_bytes < plan.bytes) return fail(TS_ENOSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, plan.bytes);
+  if (!workspace || !aligned16(workspace)) return fail(TS_EINVAL, "workspace must be 16-byte aligned memory");
   hipStream_t s = static_cast<hipStream_t>(stream);
-  KvAttnParams p = {view(cache, layer), q, q_stride, q_heads, q_heads / cache->heads, R, cap, max_blocks,
-                    ts_tree_mask_words(cap), len, n, table, mask, scale * kLog2e, out, lse};
-  launch_kv_attention(p, cache->head_dim, dtype == TS_BF16, s);
+  char* ws = static_cast<char*>(workspace);
+  const KvAttnParams p = {view(cache, layer), q, q_stride, q_heads, q_heads / cache->heads, R, cap, max_blocks,
+                          ts_tree_mask_words(cap), len, n, table, mask, scale * kLog2e, out, lse, 1,
+                          reinterpret_cast<float*>(ws), reinterpret_cast<AttnStat*>(ws + plan.stats),
+                          reinterpret_cast<AttnJoin*>(ws + plan.joins)};
+  const bool bf16 = dtype == TS_BF16;
+  if (cache->head_dim == 64) launch_kv_attention_t<64>(p, plan.tile, bf16, plan.groups, s);
+  if (cache->head_dim == 128) launch_kv_attention_t<128>(p, plan.tile, bf16, plan.groups, s);
+  if (cache->head_dim == 256) launch_kv_attention_t<256>(p, plan.tile, bf16, plan.groups, s);
   TS_HIP(hipGetLastError());
   return TS_OK;
 }

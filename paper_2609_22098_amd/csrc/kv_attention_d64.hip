@@ -1,0 +1,6 @@
+// Cache attention for head_dim 64.
+#include "kv_attention_inst.hpp"
+
+namespace ts {
+template void launch_kv_attention_t<64>(const KvAttnParams&, AttnTile, bool, int, hipStream_t);
+}  // namespace ts

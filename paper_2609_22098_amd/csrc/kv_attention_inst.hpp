@@ -1,0 +1,30 @@
+// Launcher of the cache attention for one head dimension; each has its own
+// translation unit so that they compile in parallel.
+#pragma once
+
+#include "kv_attention_kernels.hpp"
+#include "kv_launch.hpp"
+
+namespace ts {
+
+template <typename S>
+static void launch_attention_shape(const KvAttnParams& p, int groups, hipStream_t s) {
+  hipLaunchKernelGGL((kv_attention_kernel<S>), dim3(groups), dim3(S::kThreads), 0, s, p);
+  hipLaunchKernelGGL((kv_join_kernel<typename S::TE, S::D>), dim3(groups, S::kRows <= 16 ? S::kRows / 4 : 8), dim3(kJoinThreads), 0, s,
+                     p, S::kRows);
+}
+
+template <int D>
+void launch_kv_attention_t(const KvAttnParams& p, AttnTile tile, bool bf16, int groups, hipStream_t s) {
+  if (bf16) {
+    if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, __bf16>>(p, groups, s);
+    if (tile == AttnTile::k32) launch_attention_shape<AttnShape<D, 2, 1, 4, __bf16>>(p, groups, s);
+    if (tile == AttnTile::k64) launch_attention_shape<AttnShape<D, 2, 2, 2, __bf16>>(p, groups, s);
+    if (tile == AttnTile::k128) launch_attention_shape<AttnShape<D, 2, 4, 1, __bf16>>(p, groups, s);
+  } else {
+    if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, float>>(p, groups, s);
+    if (tile == AttnTile::k64) launch_attention_shape<AttnShape<D, 1, 4, 1, float>>(p, groups, s);
+  }
+}
+
+}  // namespace ts

@@ -2,97 +2,624 @@
 //
 // out = sum_t w_t V_t / sum_t w_t with w_t = exp(scale <Q, K_t> - max), in one
 // pass over the tokens with a running maximum.
+//
+// Rows.  The query heads of a group share a kv head, so the rows of a product
+// are (tree row, head of the group) pairs: row m = i * group + g of request q
+// and kv head h.  A workgroup takes a tile of them.
+//
+// Scores.  S^T = K Q^T on the scaled matrix instruction 16x16x128: its A operand
+// is the cache as it lies (16 tokens, 32 E2M1 codes and their scale byte a
+// lane), so keys are never unpacked.  Its B operand has 8 bits: a query is
+// scaled by a power of two to [128, 256) at its largest and cut into two E4M3
+// pieces of 4 significant bits each, the second holding what the first left, at
+// 2^-4 of its scale: together all 8 bits of a bf16.  That instruction drops up to
+// 2^-15 of the sum of a dot product's magnitudes, which an fp32 query would
+// show; fp32 queries take three bf16 pieces and keys unpacked to bf16 (exact).
+//
+// Values.  O^T = V^T P^T on 16x16x32 bf16 (a value of the cache is exact in
+// bf16).  Values are unpacked once per workgroup into LDS, [token][element],
+// and read back transposed.  The scores' layout (a lane holds four consecutive
+// tokens of one query) is the B operand's, so weights never leave their lane.
+// An fp32 weight is cut into three bf16 pieces, a weight for bf16 outputs is
+// rounded to one: its error is then as the output's own rounding.
+//
+// Work.  The steps of all tiles of all requests, in one line, are cut into
+// equal pieces, one a workgroup: no length decides the balance.  A tile
+// that a cut goes through leaves partial results, and a second kernel joins them.
 #pragma once
 
 #include "kv_format.hpp"
 
 namespace ts {
 
-__device__ __forceinline__ float kv_load(const float* x) { return *x; }
-__device__ __forceinline__ float kv_load(const __bf16* x) { return (float)*x; }
-__device__ __forceinline__ void kv_store(float* x, float v) { *x = v; }
-__device__ __forceinline__ void kv_store(__bf16* x, float v) { *x = (__bf16)v; }
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// A wave per (request, row, query head): 64 tokens at a time, first a lane to
-// a token for the scores, then a lane to D / 64 elements for the sums.
-constexpr int kAttnWaves = 4;
+// A tile of 16 * MB * WM rows; WT waves take token tiles in turn, WM waves share
+// one of them.
+template <int D_, int MB_, int WM_, int WT_, typename TE_>
+struct AttnShape {
+  static constexpr int D = D_, MB = MB_, WM = WM_, WT = WT_;
+  using TE = TE_;
+  static constexpr bool kF32 = sizeof(TE) == 4;
+  static constexpr int kThreads = 64 * WM * WT;
+  static constexpr int kTile = 64;               // tokens
+  static constexpr int kRows = 16 * MB * WM;     // of a workgroup's tile
+  static constexpr int kQ = kF32 ? 3 : 2;        // pieces of a query
+  static constexpr int kP = kF32 ? 3 : 1;        // pieces of a weight
+  static constexpr int kKSteps = D <= 128 ? 1 : D / 128;
+  static constexpr int kVRow = 2 * D + 32;       // bytes of a token in LDS: 4 rows of a transposed read on 32 banks
+  static constexpr int kVTokens = WM == 1 ? 32 : 128;  // a wave's half tile; two whole tiles where waves share
+  static constexpr int kORow = D + 4;            // floats of a row of results in LDS
+  static constexpr int kVBytes = WT * kVTokens * kVRow;
+  static constexpr int kOBytes = WT * WM * 16 * kORow * 4;
+  static constexpr int kLds = kVBytes > kOBytes ? kVBytes : kOBytes;
+};
+
+// A wave's 16 queries as the score products' B operand (lane: query `col`, 32
+// elements of each 128).
+template <typename S, bool F32 = S::kF32>
+struct AttnQuery;
+
+template <typename S>
+struct AttnQuery<S, false> {
+  i32x8 w[S::kKSteps][2];
+
+  // Returns what a product's score is multiplied by to give base-2 units.
+  __device__ __forceinline__ float load(const __bf16* x, bool there, int quarter, float scale_log2) {
+    float v[S::kKSteps][32];
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < S::kKSteps; ++k)
+#pragma unroll
+      for (int e = 0; e < 32; e += 8) {
+        const int d = k * 128 + (e / 16) * 64 + quarter * 16 + e % 16;  // the instruction's order of 8-bit elements
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (there && d < S::D) load8(x + d, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[k][e + j] = y[j];
+          top = max(top, __float_as_uint(y[j]) & 0x7FFFFFFFu);
+        }
+      }
+    top = max(top, (uint32_t)xor16_i32((int)top));
+    top = max(top, (uint32_t)xor32_i32((int)top));
+    const int e = max((int)(top >> 23), 8);  // x * 2^(134 - e) has its largest in [128, 256)
+    const float up = (scale_log2 < 0.f ? -1.f : 1.f) * __uint_as_float((uint32_t)(261 - e) << 23);
+#pragma unroll
+    for (int k = 0; k < S::kKSteps; ++k)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = v[k][4 * u + j] * up;
+        int word = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        word = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], word, true);
+        w[k][0][u] = word;
+        y[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(word, 0)) * 16.f;
+        y[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(word, 1)) * 16.f;
+        y[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(word, 2)) * 16.f;
+        y[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(word, 3)) * 16.f;
+        word = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        w[k][1][u] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], word, true);
+      }
+    // never 0, so that a hidden score's -inf stays one
+    return fmaxf(__builtin_fabsf(scale_log2) * __uint_as_float((uint32_t)max(e - 7, 1) << 23), 1e-36f);
+  }
+
+  __device__ __forceinline__ f32x4 scores(i32x4 codes, int scale, int k, f32x4 acc) const {
+    const i32x8 a = {codes[0], codes[1], codes[2], codes[3], 0, 0, 0, 0};
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][1], acc, 4, 0, 0, scale, 0, 127 - 4);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][0], acc, 4, 0, 0, scale, 0, 127);
+  }
+};
+
+template <typename S>
+struct AttnQuery<S, true> {
+  bf16x8 w[S::kKSteps][4][3];
+
+  __device__ __forceinline__ float load(const float* x, bool there, int quarter, float scale_log2) {
+#pragma unroll
+    for (int k = 0; k < S::kKSteps; ++k)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int d = k * 128 + quarter * 32 + u * 8;
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (there && d < S::D) load8(x + d, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float left = scale_log2 < 0.f ? -y[j] : y[j];
+#pragma unroll
+          for (int piece = 0; piece < 3; ++piece) {
+            w[k][u][piece][j] = (__bf16)left;
+            left -= (float)w[k][u][piece][j];
+          }
+        }
+      }
+    return fmaxf(__builtin_fabsf(scale_log2), 1e-36f);
+  }
+
+  __device__ __forceinline__ f32x4 scores(i32x4 codes, int scale, int k, f32x4 acc) const {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      bf16x2 y[4];
+      fp4_to_bf16x8((uint32_t)codes[u], (uint32_t)scale, y);
+      u32x4 a;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) a[j] = scale == 255 ? 0x7FC07FC0u : __builtin_bit_cast(uint32_t, y[j]);
+#pragma unroll
+      for (int piece = 2; piece >= 0; --piece)  // small ones first
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), w[k][u][piece], acc, 0, 0, 0);
+    }
+    return acc;
+  }
+};
+
+// One request's part in the line of steps.
+struct AttnReq {
+  int len, rows, tiles, steps;  // context, new rows, row tiles per kv head, steps of a tile
+};
+template <typename S>
+__device__ __forceinline__ AttnReq attn_req(const KvAttnParams& p, int q) {
+  const KvRows x = kv_rows(p.len, p.n, q, p.cap, p.max_blocks << p.c.page_shift);
+  const int step = S::kTile * S::WT;
+  return {x.len, x.rows, (x.rows * p.group + S::kRows - 1) / S::kRows, (x.len + x.rows + step - 1) / step};
+}
+
+// Workgroup sum of 64-bit counts (all threads get it), through LDS.
+template <int THREADS>
+__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  int64_t s = 0;
+  for (int w = 0; w < THREADS / 64; ++w) s += lds[w];
+  return s;
+}
+
+// Eight elements of a finished row m of (request, kv head), and its log-sum-exp.
 template <typename TE, int D>
-__global__ __launch_bounds__(64 * kAttnWaves) void kv_attention_kernel(KvAttnParams p) {
-  __shared__ float q_lds[kAttnWaves][D], w_lds[kAttnWaves][64];
-  __shared__ int page_lds[kAttnWaves][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * kAttnWaves + wave;
-  if (item >= (int64_t)p.R * p.cap * p.q_heads) return;
-  const int a = (int)(item % p.q_heads), i = (int)(item / p.q_heads % p.cap), q = (int)(item / p.q_heads / p.cap);
-  const int shift = p.c.page_shift, limit = p.max_blocks << shift;
-  const KvRows x = kv_rows(p.len, p.n, q, p.cap, limit);
-  if (i >= x.rows) return;
-  const int head = a / p.group;
-  const int32_t* table = p.table + (size_t)q * p.max_blocks;
-  const TE* qr = static_cast<const TE*>(p.q) + ((int64_t)q * p.cap + i) * p.q_stride + a * D;
-  for (int d = lane; d < D; d += 64) q_lds[wave][d] = kv_load(qr + d);
-  wave_lds_sync();
-  const uint32_t* bits = p.mask ? p.mask + ((size_t)q * p.cap + i) * p.mask_words : nullptr;
-  const int total = x.len + (bits ? x.rows : i + 1);
-  float m = kNegInf, l = 0.f, o[D / 64];
-  for (float& v : o) v = 0.f;
-  for (int t0 = 0; t0 < total; t0 += 64) {
-    const int t = t0 + lane, j = t - x.len;
-    const bool sees = t < total && (j < 0 || !bits || (bits[j >> 5] >> (j & 31) & 1u));
-    const int page = sees ? kv_page(table, t >> shift, p.max_blocks, p.c.num_pages) : -1;
-    const int off = t & ((1 << shift) - 1);
-    float s = kNegInf;
-    if (sees) {
-      s = __builtin_nanf("");
-      if (page >= 0) {
-        const char* b = kv_block<D>(p.c, page, head);
-        s = 0.f;
-        for (int g = 0; g < D / 32; ++g) {
-          const uint32_t sc = (uint8_t)b[KvBlock<D>::key_scales(off, shift) + g];
-          float dot = 0.f;
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t codes = *reinterpret_cast<const uint32_t*>(b + KvBlock<D>::key_codes(off) + g * 16 + w * 4);
-            bf16x2 k[4];
-            fp4_to_bf16x8(codes, sc == 255 ? 127u : sc, k);
-            for (int e = 0; e < 4; ++e) {
-              dot = __builtin_fmaf(q_lds[wave][g * 32 + w * 8 + 2 * e], (float)k[e][0], dot);
-              dot = __builtin_fmaf(q_lds[wave][g * 32 + w * 8 + 2 * e + 1], (float)k[e][1], dot);
+__device__ __forceinline__ void attn_out(const KvAttnParams& p, int q, int head, int m, int d, float top, float l,
+                                         const float (&y)[8]) {
+  const int i = m / p.group, a = head * p.group + (m - i * p.group);
+  const int64_t row = ((int64_t)q * p.cap + i) * p.q_heads + a;
+  TE* out = static_cast<TE*>(p.out) + row * D + d;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (sizeof(TE) == 2) {
+    bf16x8 z;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[k] = (__bf16)(y[k] * inv);
+    *reinterpret_cast<bf16x8*>(out) = z;
+  } else {
+    f32x4 z0, z1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z0[k] = y[k] * inv, z1[k] = y[k + 4] * inv;
+    *reinterpret_cast<f32x4*>(out) = z0;
+    *reinterpret_cast<f32x4*>(out + 4) = z1;
+  }
+  if (p.lse && d == 0) p.lse[row] = l == 0.f ? kNegInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams p) {
+  constexpr int D = S::D, MB = S::MB, WM = S::WM, WT = S::WT;
+  using TE = typename S::TE;
+  __shared__ __align__(16) char lds[S::kLds];
+  __shared__ float m_lds[WT][S::kRows], l_lds[WT][S::kRows];
+  __shared__ int64_t sum_lds[S::kThreads / 64];
+  __shared__ int found;
+  __shared__ int64_t found_at;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wt = wave / WM;
+  const int col = lane & 15, quarter = lane >> 4;
+  const int shift = p.c.page_shift, in_page = (1 << shift) - 1;
+
+  // The workgroup's piece of the line: workgroups of one XCD (every eighth)
+  // take neighbouring pieces, so that row tiles of one request share its L2.
+  const int groups = gridDim.x, per_xcd = groups / 8;
+  const int w = (int)blockIdx.x < per_xcd * 8 ? (blockIdx.x % 8) * per_xcd + blockIdx.x / 8 : blockIdx.x;
+  int64_t mine = 0;
+  for (int q = tid; q < p.R; q += S::kThreads) {
+    const AttnReq r = attn_req<S>(p, q);
+    mine += (int64_t)r.tiles * r.steps;
+  }
+  const int64_t total = block_sum<S::kThreads>(mine, sum_lds) * p.c.heads;
+  const int64_t per = max((total + groups - 1) / groups, (int64_t)p.min_steps);
+  const int64_t begin = per * w, end = min(begin + per, total);
+  if (tid == 0) p.joins[w].q = -1;
+  if (begin >= end) return;
+  // the request in which the piece begins
+  int64_t before = 0;
+  int q = 0;
+  for (int q0 = 0; q0 < p.R; q0 += S::kThreads) {
+    int64_t v = 0;
+    if (q0 + tid < p.R) {
+      const AttnReq r = attn_req<S>(p, q0 + tid);
+      v = (int64_t)r.tiles * r.steps * p.c.heads;
+    }
+    int64_t incl = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t x = __shfl_up(incl, d);
+      if (lane >= d) incl += x;
+    }
+    __syncthreads();
+    if (lane == 63) sum_lds[wave] = incl;
+    __syncthreads();
+    int64_t all = 0;
+    for (int u = 0; u < S::kThreads / 64; ++u) {
+      if (u < wave) incl += sum_lds[u];
+      all += sum_lds[u];
+    }
+    if (before + all > begin) {
+      if (before + incl - v <= begin && begin < before + incl) {
+        found = q0 + tid;
+        found_at = before + incl - v;
+      }
+      break;
+    }
+    before += all;
+  }
+  __syncthreads();
+  q = __builtin_amdgcn_readfirstlane(found);
+  int64_t at = found_at;  // of request q's first step
+
+  const int g_rows = p.group;
+  for (int64_t pos = begin; pos < end;) {
+    AttnReq r = attn_req<S>(p, q);
+    const int64_t of_q = (int64_t)r.tiles * r.steps * p.c.heads;
+    if (pos >= at + of_q) {
+      at += of_q;
+      ++q;
+      continue;
+    }
+    const int item = (int)((pos - at) / r.steps);
+    const int64_t item_at = at + (int64_t)item * r.steps;
+    const int s0 = (int)(pos - item_at), s1 = (int)min(end - item_at, (int64_t)r.steps);
+    const int head = item / r.tiles, rt = item % r.tiles;
+    const int rows_m = r.rows * g_rows, m0 = rt * S::kRows;
+    const int context = r.len, all_tokens = r.len + r.rows;
+    const int32_t* table = p.table + (size_t)q * p.max_blocks;
+
+    // ---- queries
+    AttnQuery<S> qp[MB];
+    float c_row[MB];
+    int row_i[MB];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      const int m = m0 + (wm * MB + b) * 16 + col;
+      const bool there = m < rows_m;
+      const int i = there ? m / g_rows : 0, g = there ? m - i * g_rows : 0;
+      row_i[b] = there ? i : -1;
+      const TE* x = static_cast<const TE*>(p.q) + ((int64_t)q * p.cap + i) * p.q_stride + (head * g_rows + g) * D;
+      c_row[b] = qp[b].load(x, there, quarter, p.scale_log2);
+    }
+
+    // ---- tokens
+    float m_run[MB], l_run[MB];
+    f32x4 o[MB][D / 16];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      m_run[b] = kNegInf, l_run[b] = 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // last position that a row of the tile sees, and so the last step
+    const int i_last = min((m0 + S::kRows - 1) / g_rows, r.rows - 1);
+    const int need = p.mask ? all_tokens : context + i_last + 1;
+
+    constexpr int kVLoads = D / 32;  // of a token tile, 16 bytes a lane
+    constexpr int kVMine = (kVLoads + WM - 1) / WM;
+    struct Tile {
+      i32x4 k[4][S::kKSteps];
+      int ks[4][S::kKSteps];
+      u32x4 v[kVMine];
+      uint32_t vs[kVMine];
+    };
+    // the four pages of a tile's runs of 16 tokens
+    auto pages_of = [&](int step, int (&pg)[4]) {
+      const int t0 = (step * WT + wt) * S::kTile;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = t0 + 16 * u;
+        pg[u] = t < need ? kv_page(table, t >> shift, p.max_blocks, p.c.num_pages) : -1;
+      }
+    };
+    auto load = [&](int step, const int (&pg_)[4], Tile& x) {
+      const int t0 = (step * WT + wt) * S::kTile;
+      int pg[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) pg[u] = __builtin_amdgcn_readfirstlane(pg_[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int off = ((t0 + 16 * u) & in_page) + col;
+        const char* blk = kv_block<D>(p.c, max(pg[u], 0), head);
+#pragma unroll
+        for (int k = 0; k < S::kKSteps; ++k) {
+          // a run without a page has scale 255: its scores are not-a-number
+          x.k[u][k] = i32x4{0, 0, 0, 0};
+          x.ks[u][k] = pg[u] < 0 ? 255 : 127;
+          if (pg[u] >= 0 && (D >= 128 || quarter < 2)) {
+            x.k[u][k] = *reinterpret_cast<const i32x4*>(blk + KvBlock<D>::key_codes(off) + k * 64 + quarter * 16);
+            x.ks[u][k] = (uint8_t)blk[KvBlock<D>::key_scales(off, shift) + k * 4 + quarter];
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kVMine; ++j) {
+        const int piece = (j * WM + wm) * 64 + lane;  // in the tile's 2 D pieces of 32 elements
+        const int tok = piece / (D / 32), part = piece % (D / 32);
+        x.v[j] = u32x4{0, 0, 0, 0};
+        x.vs[j] = 127;
+        const int run = tok >> 4;
+        const int page = run == 0 ? pg[0] : run == 1 ? pg[1] : run == 2 ? pg[2] : pg[3];
+        if (j * WM + wm < kVLoads && page >= 0) {
+          const int off = (t0 + tok) & in_page;
+          const char* blk = kv_block<D>(p.c, page, head);
+          x.v[j] = *reinterpret_cast<const u32x4*>(blk + KvBlock<D>::value_codes(off, shift) + part * 16);
+          x.vs[j] = (uint8_t)blk[KvBlock<D>::value_scales(off, shift) + part];
+        }
+      }
+    };
+    // unpack a load's values into LDS, at the tile's token `tok - first`
+    auto unpack = [&](const Tile& x, int j, char* to, int first) {
+      const int piece = (j * WM + wm) * 64 + lane;
+      const int tok = piece / (D / 32) - first, part = piece % (D / 32);
+      if (j * WM + wm >= kVLoads) return;
+      const uint32_t sc = value_scale(x.vs[j]);
+      const bool none = x.vs[j] == 255;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        bf16x2 y[4];
+        fp4_to_bf16x8(none ? 0u : x.v[j][u], sc, y);
+        u32x4 z;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] = __builtin_bit_cast(uint32_t, y[k]);
+        *reinterpret_cast<u32x4*>(to + tok * S::kVRow + part * 64 + u * 16) = z;
+      }
+    };
+
+    Tile cur, next;
+    int pg[4];
+    pages_of(s0, pg);
+    load(s0, pg, cur);
+    pages_of(s0 + 1, pg);
+    char* v_lds = lds + wt * (S::kVTokens * S::kVRow);
+    for (int s = s0; s < s1; ++s) {
+      if (s + 1 < s1) {
+        load(s + 1, pg, next);
+        pages_of(s + 2, pg);
+      }
+      const int t0 = (s * WT + wt) * S::kTile;
+      char* v_tile = v_lds;
+      if constexpr (WM > 1) {
+        v_tile += ((s - s0) & 1) * (64 * S::kVRow);
+#pragma unroll
+        for (int j = 0; j < kVMine; ++j) unpack(cur, j, v_tile, 0);
+        __syncthreads();  // and every wave is done with the tile before the last
+      }
+      if (t0 < need) {
+        // scores
+        f32x4 sc[MB][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int b = 0; b < MB; ++b) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < S::kKSteps; ++k) {
+              acc = qp[b].scores(cur.k[u][k], cur.ks[u][k], k, acc);
+            }
+            sc[b][u] = acc;
+          }
+        if (t0 + S::kTile > context) {  // the tile holds new rows or ends
+#pragma unroll
+          for (int b = 0; b < MB; ++b) {
+            uint64_t sees = 0;
+            const int i = row_i[b], j0 = t0 - context;
+            if (i >= 0) {
+              if (!p.mask) {
+                const int cnt = min(max(i + 1 - j0, 0), 64);
+                sees = cnt == 64 ? ~0ull : (1ull << cnt) - 1;
+              } else {
+                const uint32_t* bits = p.mask + ((size_t)q * p.cap + i) * p.mask_words;
+                const int first = max(j0, 0), w0 = first >> 5, sh = first & 31;
+                uint32_t word[3];
+#pragma unroll
+                for (int u = 0; u < 3; ++u) word[u] = w0 + u < p.mask_words ? bits[w0 + u] : 0u;
+                uint64_t win = (((uint64_t)word[1] << 32) | word[0]) >> sh;
+                if (sh) win |= (uint64_t)word[2] << (64 - sh);
+                if (j0 < 0) win = j0 > -64 ? (win << -j0) | ((1ull << -j0) - 1) : ~0ull;
+                const int cnt = min(all_tokens - t0, 64);
+                sees = cnt >= 64 ? win : win & ((1ull << cnt) - 1);
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const uint32_t four = (uint32_t)(sees >> (16 * u + 4 * quarter)) & 15u;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sc[b][u][e] = four >> e & 1 ? sc[b][u][e] : kNegInf;
             }
           }
-          s += sc == 255 ? __builtin_nanf("") : dot;
         }
-        s *= p.scale_log2;
+        // weights
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+          float top = kNegInf;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[b][u][e]);
+          top = fmaxf(top, xor16_f32(top));
+          top = fmaxf(top, xor32_f32(top));
+          top *= c_row[b];
+          if (__any(top > m_run[b])) {
+            const float m_new = fmaxf(m_run[b], top);
+            const float keep = m_new == kNegInf ? 1.f : exp2_fast(m_run[b] - m_new);
+            m_run[b] = m_new;
+            l_run[b] *= keep;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) o[b][d] *= keep;
+          }
+          const float sub = m_run[b] == kNegInf ? 0.f : m_run[b];
+          float sum = 0.f;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              sc[b][u][e] = exp2_fast(__builtin_fmaf(sc[b][u][e], c_row[b], -sub));
+              sum += sc[b][u][e];
+            }
+          l_run[b] += sum;
+        }
+        // values
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const char* from = v_tile + (WM == 1 ? 0 : half * 32 * S::kVRow);
+          if constexpr (WM == 1) {
+#pragma unroll
+            for (int j = 0; j < kVMine / 2; ++j) unpack(cur, half * (kVMine / 2) + j, v_tile, half * 32);
+            wave_lds_sync();
+          }
+          bf16x8 w8[MB][S::kP];
+#pragma unroll
+          for (int b = 0; b < MB; ++b)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float left = sc[b][2 * half + e / 4][e % 4];
+#pragma unroll
+              for (int piece = 0; piece < S::kP; ++piece) {
+                w8[b][piece][e] = (__bf16)left;
+                left -= (float)w8[b][piece][e];
+              }
+            }
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) {
+            typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+            const char* a = from + (4 * quarter + col / 4) * S::kVRow + d * 32 + (col % 4) * 8;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a + 16 * S::kVRow));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+              for (int piece = S::kP - 1; piece >= 0; --piece)
+                o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), w8[b][piece], o[b][d], 0, 0, 0);
+          }
+          if constexpr (WM == 1) wave_lds_sync();
+        }
+      }
+      if (s + 1 < s1) cur = next;
+    }
+
+    // ---- join the waves, and out
+    const bool whole = s0 == 0 && s1 == r.steps;
+    const int slot = 2 * w + (pos == begin ? 0 : 1);
+    __syncthreads();  // values in LDS have been read
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      l_run[b] = cross_row_sum(l_run[b]);
+      if (quarter == 0) {
+        m_lds[wt][(wm * MB + b) * 16 + col] = m_run[b];
+        l_lds[wt][(wm * MB + b) * 16 + col] = l_run[b];
       }
     }
-    const float top = fmaxf(m, wave_max(s));
-    const float at = top == kNegInf ? 0.f : top;
-    const float w = sees ? exp2_fast(s - at) : 0.f, keep = exp2_fast(m - at);
-    l = l * keep + wave_sum(w);
-    m = top;
-    w_lds[wave][lane] = w;
-    page_lds[wave][lane] = page;
-    wave_lds_sync();
-    for (float& v : o) v *= keep;
-    for (int u = 0; u < min(64, total - t0); ++u) {
-      const int pg = page_lds[wave][u], of = (t0 + u) & ((1 << shift) - 1);
-      if (pg < 0) continue;
-      const char* b = kv_block<D>(p.c, pg, head);
-      const float wu = w_lds[wave][u];
-      for (int e = 0; e < D / 64; ++e) {
-        const int d = lane + 64 * e;
-        const uint32_t sc = (uint8_t)b[KvBlock<D>::value_scales(of, shift) + d / 32];
-        const uint32_t code = (uint8_t)b[KvBlock<D>::value_codes(of, shift) + d / 2];
-        bf16x2 v[4];
-        fp4_to_bf16x8(sc == 255 ? 0u : code, value_scale(sc), v);
-        o[e] = __builtin_fmaf(wu, (float)v[0][d & 1], o[e]);
+    __syncthreads();
+    float* o_lds = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      const int mine_row = (wm * MB + b) * 16 + col;
+      float top = kNegInf;
+#pragma unroll
+      for (int u = 0; u < WT; ++u) top = fmaxf(top, m_lds[u][mine_row]);
+      const float keep = top == kNegInf ? 1.f : exp2_fast(m_run[b] - top);
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d)
+        *reinterpret_cast<f32x4*>(o_lds + ((wt * WM + wm) * 16 + col) * S::kORow + d * 16 + quarter * 4) = o[b][d] * keep;
+      __syncthreads();
+      for (int x = tid; x < WM * 16 * (D / 8); x += S::kThreads) {
+        const int row = x / (D / 8), d = x % (D / 8) * 8;  // row: of the waves' blocks b
+        const int m_in = ((row / 16) * MB + b) * 16 + row % 16, m = m0 + m_in;
+        if (m >= rows_m) continue;
+        float top2 = kNegInf;
+#pragma unroll
+        for (int u = 0; u < WT; ++u) top2 = fmaxf(top2, m_lds[u][m_in]);
+        float l = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < WT; ++u) {
+          l += l_lds[u][m_in] * (top2 == kNegInf ? 1.f : exp2_fast(m_lds[u][m_in] - top2));
+          const float* z = o_lds + (u * WM * 16 + row) * S::kORow + d;
+          const f32x4 z0 = *reinterpret_cast<const f32x4*>(z), z1 = *reinterpret_cast<const f32x4*>(z + 4);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] += z0[k], y[k + 4] += z1[k];
+        }
+        if (whole) {
+          attn_out<TE, D>(p, q, head, m, d, top2, l, y);
+        } else {
+          float* part = p.parts + ((size_t)slot * S::kRows + m_in) * D + d;
+          *reinterpret_cast<f32x4*>(part) = f32x4{y[0], y[1], y[2], y[3]};
+          *reinterpret_cast<f32x4*>(part + 4) = f32x4{y[4], y[5], y[6], y[7]};
+          if (d == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{top2, l};
+        }
       }
+      __syncthreads();
     }
-    wave_lds_sync();
+    // the first workgroup whose piece begins inside the tile says where its parts are
+    if (tid == 0 && pos == begin && s0 > 0 && begin - per <= item_at) {
+      const int last = (int)((item_at + r.steps - 1) / per);
+      p.joins[w] = AttnJoin{q, head, m0, min(S::kRows, rows_m - m0), 2 * (w - 1) + (begin - per == item_at ? 0 : 1), last};
+    }
+    pos = item_at + s1;
   }
-  TE* out = static_cast<TE*>(p.out) + (((int64_t)q * p.cap + i) * p.q_heads + a) * D;
-  for (int e = 0; e < D / 64; ++e) kv_store(out + lane + 64 * e, l == 0.f ? 0.f : o[e] / l);
-  if (p.lse && lane == 0)
-    p.lse[((int64_t)q * p.cap + i) * p.q_heads + a] = l == 0.f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Joins the parts of a tile that more than one workgroup worked on: block
+// (w, y) rows y, y + gridDim.y, ... of the tile that joins[w] names.  Thread
+// groups of D / 4 lanes take its parts in turn.
+constexpr int kJoinThreads = 256;
+template <typename TE, int D>
+__global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(KvAttnParams p, int rows) {
+  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
+  __shared__ f32x4 o_lds[kGroups][kLanes];
+  __shared__ float l_lds[kGroups];
+  const int w = blockIdx.x;
+  const AttnJoin j = p.joins[w];
+  if (j.q < 0) return;
+  const int grp = threadIdx.x / kLanes, at = threadIdx.x % kLanes;
+  const int count = j.last - w + 2;  // parts: the first, then 2 w, 2 (w + 1), ...
+  for (int row = blockIdx.y; row < j.rows; row += gridDim.y) {
+    float top = kNegInf;
+    for (int x = 0; x < count; ++x) {
+      const int slot = x ? 2 * (w + x - 1) : j.first;
+      top = fmaxf(top, p.stats[(size_t)slot * rows + row].m);
+    }
+    float l = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int x = grp; x < count; x += kGroups) {
+      const int slot = x ? 2 * (w + x - 1) : j.first;
+      const AttnStat st = p.stats[(size_t)slot * rows + row];
+      const float keep = top == kNegInf ? 1.f : exp2_fast(st.m - top);
+      l += st.l * keep;
+      y += *reinterpret_cast<const f32x4*>(p.parts + ((size_t)slot * rows + row) * D + at * 4) * keep;
+    }
+    __syncthreads();
+    o_lds[grp][at] = y;
+    if (at == 0) l_lds[grp] = l;
+    __syncthreads();
+    if (threadIdx.x < D / 8) {
+      float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+      for (int x = 0; x < kGroups; ++x) {
+        sum += l_lds[x];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z[k] += o_lds[x][threadIdx.x * 2 + k / 4][k % 4];
+      }
+      attn_out<TE, D>(p, j.q, j.head, j.m0 + row, threadIdx.x * 8, top, sum, z);
+    }
+  }
 }
 
 }  // namespace ts

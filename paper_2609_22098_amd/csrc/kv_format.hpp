@@ -67,6 +67,21 @@ __device__ __forceinline__ void fp4_to_bf16x8(uint32_t codes, uint32_t scale_byt
 // clamp keeps every value finite (a masked one is multiplied by a weight of 0).
 __device__ __forceinline__ uint32_t value_scale(uint32_t s) { return min(s, 252u); }
 
+// Eight consecutive elements as fp32.
+__device__ __forceinline__ void load8(const float* x, float (&v)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(x), b = *reinterpret_cast<const f32x4*>(x + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = a[i], v[i + 4] = b[i];
+}
+__device__ __forceinline__ void load8(const __bf16* x, float (&v)[8]) {
+  const u32x4 a = *reinterpret_cast<const u32x4*>(x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(a[i] << 16);
+    v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+  }
+}
+
 // LDS written by lanes of a wave is read by others of the same wave: LDS works in
 // program order there, so only the compiler has to keep the order.
 __device__ __forceinline__ void wave_lds_sync() {
@@ -105,6 +120,20 @@ struct KvAcceptParams {
   int32_t* new_len;
 };
 
+// Row tiles of the attention kernel: rows of a workgroup's tile and its waves (see AttnShape).
+enum class AttnTile : int { k16, k32, k64, k128 };
+
+// A partial result's statistics: running maximum (base-2 units) and sum of weights.
+struct AttnStat {
+  float m, l;
+};
+// A row tile whose parts a second kernel joins; q < 0: none.
+struct AttnJoin {
+  int q, head, m0, rows;
+  int first;  // slot of its first part; the others are 2 w, 2 (w + 1), ...
+  int last;   // workgroup of the last part
+};
+
 struct KvAttnParams {
   KvView c;
   const void* q;
@@ -115,6 +144,10 @@ struct KvAttnParams {
   float scale_log2;  // scale * log2(e): scores in base-2 units
   void* out;
   float* lse;
+  int min_steps;   // of a workgroup
+  float* parts;    // [2 * workgroups][rows of a tile][D]
+  AttnStat* stats; // [2 * workgroups][rows of a tile]
+  AttnJoin* joins; // [workgroups]
 };
 
 }  // namespace ts

@@ -8,21 +8,6 @@ namespace ts {
 
 constexpr int kRowThreads = 256;
 
-// Eight consecutive elements as fp32.
-__device__ __forceinline__ void load8(const float* x, float (&v)[8]) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(x), b = *reinterpret_cast<const f32x4*>(x + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = a[i], v[i + 4] = b[i];
-}
-__device__ __forceinline__ void load8(const __bf16* x, float (&v)[8]) {
-  const u32x4 a = *reinterpret_cast<const u32x4*>(x);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(a[i] << 16);
-    v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
-  }
-}
-
 // Largest magnitude of a group's 32 elements, its four lanes (a quad) agreeing;
 // the bits of magnitudes order as integers do, NaN and infinity on top.
 __device__ __forceinline__ uint32_t group_max_bits(const float (&v)[8]) {

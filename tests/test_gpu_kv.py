@@ -333,7 +333,7 @@ def test_attention_unwritten_bytes(torch):
         for q in range(2):
             pos = np.arange(c.lens[q] + rows)
             used[c.table[q, pos // 64] * 64 + pos % 64] = True
-        packed = torch.from_numpy(kv_ref.pack(c.ref)[0]).view(-1, 2, 64 * 136)
+        packed = torch.from_numpy(kv_ref.pack(c.ref)[0].copy()).view(-1, 2, 64 * 136)
         for at, size in ((0, 64), (64 * 64, 4), (64 * 68, 64), (64 * 132, 4)):
             part = packed[:, :, at:at + 64 * size].unflatten(2, (64, size))
             part[~torch.from_numpy(used).view(-1, 64)[:, None, :].expand(-1, 2, -1)] = 255 if size == 64 else 254
