@@ -10,8 +10,9 @@ namespace ts {
 template <typename S>
 static void launch_attention_shape(const KvAttnParams& p, int groups, hipStream_t s) {
   hipLaunchKernelGGL((kv_attention_kernel<S>), dim3(groups), dim3(S::kThreads), 0, s, p);
-  hipLaunchKernelGGL((kv_join_kernel<typename S::TE, S::D>), dim3(groups, S::kRows <= 16 ? S::kRows / 4 : 8), dim3(kJoinThreads), 0, s,
-                     p, S::kRows);
+  const int units = groups * (S::kRows / 4);
+  hipLaunchKernelGGL((kv_join_kernel<typename S::TE, S::D>), dim3(units < kJoinBlocks ? units : kJoinBlocks), dim3(kJoinThreads), 0, s,
+                     p, __builtin_ctz(S::kRows), units);
 }
 
 template <int D>

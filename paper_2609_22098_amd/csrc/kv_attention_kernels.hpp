@@ -54,6 +54,9 @@ struct AttnShape {
   static constexpr int kORow = D + 4;            // floats of a row of results in LDS
   static constexpr int kVBytes = WT * kVTokens * kVRow;
   static constexpr int kOBytes = WT * WM * 16 * kORow * 4;
+  static constexpr int kFixed = 128 * WT;        // tokens' worth of a tile's beginning and end
+  // workgroups on a compute unit: registers allow waves of 128 where a wave has one block of rows
+  static constexpr int kResident = MB == 1 && D <= 128 && !kF32 ? 3 : D <= 128 ? 2 : 1;
   static constexpr int kLds = kVBytes > kOBytes ? kVBytes : kOBytes;
 };
 
@@ -156,29 +159,36 @@ struct AttnQuery<S, true> {
   }
 };
 
-// One request's part in the line of steps.
-struct AttnReq {
-  int len, rows, tiles, steps;  // context, new rows, row tiles per kv head, steps of a tile
-};
+// One request's part in the line.  A row tile's length in it is the number of
+// (token, query head of the group) pairs that its last row may see, and as much
+// again as its beginning and end cost: with a mask the same for all tiles; a
+// chain's tiles grow by kRows each.
 template <typename S>
-__device__ __forceinline__ AttnReq attn_req(const KvAttnParams& p, int q) {
-  const KvRows x = kv_rows(p.len, p.n, q, p.cap, p.max_blocks << p.c.page_shift);
-  const int step = S::kTile * S::WT;
-  return {x.len, x.rows, (x.rows * p.group + S::kRows - 1) / S::kRows, (x.len + x.rows + step - 1) / step};
-}
+struct AttnReq {
+  int len, rows, tiles;      // context, new rows, row tiles per kv head
+  int64_t first, more, all;  // length of tile 0, growth, sum over the tiles
 
-// Workgroup sum of 64-bit counts (all threads get it), through LDS.
-template <int THREADS>
-__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  int64_t s = 0;
-  for (int w = 0; w < THREADS / 64; ++w) s += lds[w];
-  return s;
-}
+  __device__ __forceinline__ AttnReq(const KvAttnParams& p, int q) {
+    const KvRows x = kv_rows(p.len, p.n, q, p.cap, p.max_blocks << p.c.page_shift);
+    len = x.len, rows = x.rows;
+    tiles = (rows * p.group + S::kRows - 1) / S::kRows;
+    more = p.mask ? 0 : S::kRows;
+    first = (int64_t)(len + S::kFixed) * p.group + (p.mask ? rows * p.group : S::kRows);
+    all = before(tiles);
+  }
+  // sum over the tiles before tile t
+  __device__ __forceinline__ int64_t before(int t) const { return t * first + more * ((int64_t)t * (t - 1) / 2); }
+  // the tile that holds place x < all
+  __device__ __forceinline__ int tile_at(int64_t x) const {
+    if (more == 0) return (int)(x / first);
+    int lo = 0, hi = tiles - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (before(mid) <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+  }
+};
 
 // Eight elements of a finished row m of (request, kv head), and its log-sum-exp.
 template <typename TE, int D>
@@ -204,7 +214,7 @@ __device__ __forceinline__ void attn_out(const KvAttnParams& p, int q, int head,
 }
 
 template <typename S>
-__global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams p) {
+__global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel(KvAttnParams p) {
   constexpr int D = S::D, MB = S::MB, WM = S::WM, WT = S::WT;
   using TE = typename S::TE;
   __shared__ __align__(16) char lds[S::kLds];
@@ -221,25 +231,9 @@ __global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams 
   // take neighbouring pieces, so that row tiles of one request share its L2.
   const int groups = gridDim.x, per_xcd = groups / 8;
   const int w = (int)blockIdx.x < per_xcd * 8 ? (blockIdx.x % 8) * per_xcd + blockIdx.x / 8 : blockIdx.x;
-  int64_t mine = 0;
-  for (int q = tid; q < p.R; q += S::kThreads) {
-    const AttnReq r = attn_req<S>(p, q);
-    mine += (int64_t)r.tiles * r.steps;
-  }
-  const int64_t total = block_sum<S::kThreads>(mine, sum_lds) * p.c.heads;
-  const int64_t per = max((total + groups - 1) / groups, (int64_t)p.min_steps);
-  const int64_t begin = per * w, end = min(begin + per, total);
-  if (tid == 0) p.joins[w].q = -1;
-  if (begin >= end) return;
-  // the request in which the piece begins
-  int64_t before = 0;
-  int q = 0;
-  for (int q0 = 0; q0 < p.R; q0 += S::kThreads) {
-    int64_t v = 0;
-    if (q0 + tid < p.R) {
-      const AttnReq r = attn_req<S>(p, q0 + tid);
-      v = (int64_t)r.tiles * r.steps * p.c.heads;
-    }
+  // Inclusive sum over a thread's request and those before it from q0 on.
+  auto scan = [&](int q0, int64_t& v, int64_t& all) {
+    v = q0 + tid < p.R ? AttnReq<S>(p, q0 + tid).all * p.c.heads : 0;
     int64_t incl = v;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -249,40 +243,151 @@ __global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams 
     __syncthreads();
     if (lane == 63) sum_lds[wave] = incl;
     __syncthreads();
-    int64_t all = 0;
+    all = 0;
+#pragma unroll
     for (int u = 0; u < S::kThreads / 64; ++u) {
       if (u < wave) incl += sum_lds[u];
       all += sum_lds[u];
     }
-    if (before + all > begin) {
-      if (before + incl - v <= begin && begin < before + incl) {
-        found = q0 + tid;
-        found_at = before + incl - v;
-      }
-      break;
+    return incl;
+  };
+  int64_t v, all, incl = scan(0, v, all), total = all;
+  for (int q0 = S::kThreads; q0 < p.R; q0 += S::kThreads) {
+    scan(q0, v, all);
+    total += all;
+  }
+  const int64_t per = max((total + groups - 1) / groups, (int64_t)p.min_tokens * p.group);
+  const int64_t begin = per * w, end = min(begin + per, total);
+  if (tid == 0) p.joins[w].q = -1;
+  if (begin >= end) return;
+  int64_t before = 0;
+  for (int q0 = 0; q0 < p.R; q0 += S::kThreads) {
+    if (p.R > S::kThreads) incl = scan(q0, v, all);
+    if (before + incl - v <= begin && begin < before + incl) {
+      found = q0 + tid;
+      found_at = before + incl - v;
     }
     before += all;
   }
   __syncthreads();
-  q = __builtin_amdgcn_readfirstlane(found);
+  int q = __builtin_amdgcn_readfirstlane(found);
   int64_t at = found_at;  // of request q's first step
 
   const int g_rows = p.group;
   for (int64_t pos = begin; pos < end;) {
-    AttnReq r = attn_req<S>(p, q);
-    const int64_t of_q = (int64_t)r.tiles * r.steps * p.c.heads;
-    if (pos >= at + of_q) {
-      at += of_q;
+    const AttnReq<S> r(p, q);
+    if (pos >= at + r.all * p.c.heads) {
+      at += r.all * p.c.heads;
       ++q;
       continue;
     }
-    const int item = (int)((pos - at) / r.steps);
-    const int64_t item_at = at + (int64_t)item * r.steps;
-    const int s0 = (int)(pos - item_at), s1 = (int)min(end - item_at, (int64_t)r.steps);
-    const int head = item / r.tiles, rt = item % r.tiles;
+    const int head = (int)((pos - at) / r.all);
+    const int rt = r.tile_at(pos - at - head * r.all);
+    const int64_t tile_at = at + head * r.all + r.before(rt), tile_len = r.first + r.more * rt, tile_end = tile_at + tile_len;
     const int rows_m = r.rows * g_rows, m0 = rt * S::kRows;
     const int context = r.len, all_tokens = r.len + r.rows;
     const int32_t* table = p.table + (size_t)q * p.max_blocks;
+
+    // ---- tokens
+    float m_run[MB], l_run[MB];
+    f32x4 o[MB][D / 16];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      m_run[b] = kNegInf, l_run[b] = 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // last position that a row of the tile sees, and so the last step
+    const int i_last = min((m0 + S::kRows - 1) / g_rows, r.rows - 1);
+    const int need = p.mask ? all_tokens : context + i_last + 1;
+    // the workgroup's steps: both sides of a cut round its place up alike
+    const int64_t steps = (need + S::kTile * WT - 1) / (S::kTile * WT);
+    const int64_t stop = min(end, tile_end);
+    const int s0 = (int)(((pos - tile_at) * steps + tile_len - 1) / tile_len);
+    const int s1 = (int)(((stop - tile_at) * steps + tile_len - 1) / tile_len);
+
+    constexpr int kVLoads = D / 32;  // of a token tile, 16 bytes a lane
+    constexpr int kVMine = (kVLoads + WM - 1) / WM;
+    i32x4 kc[4][S::kKSteps];  // keys: codes and scales of the lane's token in each run of 16
+    int ks[4][S::kKSteps];
+    u32x4 vc[kVMine];         // values
+    uint32_t vs[kVMine];
+    // The pages of a tile's runs of 16 tokens, -1 where there is none.
+    auto pages_of = [&](int step, int (&pg)[4]) {
+      const int t0 = (step * WT + wt) * S::kTile;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int blk = (t0 + 16 * u) >> shift;
+        const int page = table[min(blk, p.max_blocks - 1)];
+        pg[u] = blk < p.max_blocks && (uint32_t)page < (uint32_t)p.c.num_pages ? page : -1;
+      }
+    };
+    // Loads of runs without a page go to page 0 and are set aside: keys get
+    // scale 255, so that their scores are not-a-number, values read as zero.
+    auto load_keys = [&](int step, const int (&pg)[4]) {
+      const int t0 = (step * WT + wt) * S::kTile;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const char* blk = kv_block<D>(p.c, max(pg[u], 0), head);
+        const int off = ((t0 + 16 * u) & in_page) + col;
+#pragma unroll
+        for (int k = 0; k < S::kKSteps; ++k) {
+          const int part = D >= 128 ? k * 4 + quarter : quarter & 1;
+          kc[u][k] = *reinterpret_cast<const i32x4*>(blk + (uint32_t)(KvBlock<D>::key_codes(off) + part * 16));
+          ks[u][k] = (uint8_t)blk[(uint32_t)(KvBlock<D>::key_scales(off, shift) + part)];
+        }
+      }
+    };
+    auto load_values = [&](int step, const int (&pg)[4]) {
+      const int t0 = (step * WT + wt) * S::kTile;
+#pragma unroll
+      for (int j = 0; j < kVMine; ++j) {
+        const int piece = (j * WM + wm) * 64 + lane;  // in the tile's 2 D pieces of 32 elements
+        const int tok = piece / (D / 32), part = piece % (D / 32), off = (t0 + tok) & in_page;
+        // a load covers 512 / (D / 4) tokens: one run of 16, half of one or two
+        int page;
+        if constexpr (D == 64) {
+          const int run = min((j * WM + wm) * 2, 2);
+          page = lane < 32 ? pg[0] : pg[1];
+          if (run) page = lane < 32 ? pg[2] : pg[3];
+        } else {
+          const int run = min((j * WM + wm) * 128 / D, 3);
+          page = run == 0 ? pg[0] : run == 1 ? pg[1] : run == 2 ? pg[2] : pg[3];
+        }
+        if (j * WM + wm < kVLoads) {
+          const char* blk = kv_block<D>(p.c, max(page, 0), head);
+          vc[j] = *reinterpret_cast<const u32x4*>(blk + (uint32_t)(KvBlock<D>::value_codes(off, shift) + part * 16));
+          vs[j] = page < 0 ? 255u : (uint8_t)blk[(uint32_t)(KvBlock<D>::value_scales(off, shift) + part)];
+        }
+      }
+    };
+    // unpack a load's values into LDS, at the tile's token `tok - first`
+    auto unpack = [&](int j, char* to, int first) {
+      const int piece = (j * WM + wm) * 64 + lane;
+      const int tok = piece / (D / 32) - first, part = piece % (D / 32);
+      if (j * WM + wm >= kVLoads) return;
+      const uint32_t sc = value_scale(vs[j]);
+      const bool none = vs[j] == 255;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        bf16x2 y[4];
+        fp4_to_bf16x8(none ? 0u : vc[j][u], sc, y);
+        u32x4 z;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] = __builtin_bit_cast(uint32_t, y[k]);
+        *reinterpret_cast<u32x4*>(to + tok * S::kVRow + part * 64 + u * 16) = z;
+      }
+    };
+
+    // Each register is loaded again for the next step as soon as this one is
+    // done with it; pages are looked up a step earlier.
+    int pg[4], pg_next[4];
+    pages_of(s0, pg);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) pg[u] = __builtin_amdgcn_readfirstlane(pg[u]);
+    load_keys(s0, pg);
+    load_values(s0, pg);
+    pages_of(s0 + 1, pg_next);
 
     // ---- queries
     AttnQuery<S> qp[MB];
@@ -298,107 +403,19 @@ __global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams 
       c_row[b] = qp[b].load(x, there, quarter, p.scale_log2);
     }
 
-    // ---- tokens
-    float m_run[MB], l_run[MB];
-    f32x4 o[MB][D / 16];
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-      m_run[b] = kNegInf, l_run[b] = 0.f;
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    // last position that a row of the tile sees, and so the last step
-    const int i_last = min((m0 + S::kRows - 1) / g_rows, r.rows - 1);
-    const int need = p.mask ? all_tokens : context + i_last + 1;
-
-    constexpr int kVLoads = D / 32;  // of a token tile, 16 bytes a lane
-    constexpr int kVMine = (kVLoads + WM - 1) / WM;
-    struct Tile {
-      i32x4 k[4][S::kKSteps];
-      int ks[4][S::kKSteps];
-      u32x4 v[kVMine];
-      uint32_t vs[kVMine];
-    };
-    // the four pages of a tile's runs of 16 tokens
-    auto pages_of = [&](int step, int (&pg)[4]) {
-      const int t0 = (step * WT + wt) * S::kTile;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int t = t0 + 16 * u;
-        pg[u] = t < need ? kv_page(table, t >> shift, p.max_blocks, p.c.num_pages) : -1;
-      }
-    };
-    auto load = [&](int step, const int (&pg_)[4], Tile& x) {
-      const int t0 = (step * WT + wt) * S::kTile;
-      int pg[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) pg[u] = __builtin_amdgcn_readfirstlane(pg_[u]);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int off = ((t0 + 16 * u) & in_page) + col;
-        const char* blk = kv_block<D>(p.c, max(pg[u], 0), head);
-#pragma unroll
-        for (int k = 0; k < S::kKSteps; ++k) {
-          // a run without a page has scale 255: its scores are not-a-number
-          x.k[u][k] = i32x4{0, 0, 0, 0};
-          x.ks[u][k] = pg[u] < 0 ? 255 : 127;
-          if (pg[u] >= 0 && (D >= 128 || quarter < 2)) {
-            x.k[u][k] = *reinterpret_cast<const i32x4*>(blk + KvBlock<D>::key_codes(off) + k * 64 + quarter * 16);
-            x.ks[u][k] = (uint8_t)blk[KvBlock<D>::key_scales(off, shift) + k * 4 + quarter];
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kVMine; ++j) {
-        const int piece = (j * WM + wm) * 64 + lane;  // in the tile's 2 D pieces of 32 elements
-        const int tok = piece / (D / 32), part = piece % (D / 32);
-        x.v[j] = u32x4{0, 0, 0, 0};
-        x.vs[j] = 127;
-        const int run = tok >> 4;
-        const int page = run == 0 ? pg[0] : run == 1 ? pg[1] : run == 2 ? pg[2] : pg[3];
-        if (j * WM + wm < kVLoads && page >= 0) {
-          const int off = (t0 + tok) & in_page;
-          const char* blk = kv_block<D>(p.c, page, head);
-          x.v[j] = *reinterpret_cast<const u32x4*>(blk + KvBlock<D>::value_codes(off, shift) + part * 16);
-          x.vs[j] = (uint8_t)blk[KvBlock<D>::value_scales(off, shift) + part];
-        }
-      }
-    };
-    // unpack a load's values into LDS, at the tile's token `tok - first`
-    auto unpack = [&](const Tile& x, int j, char* to, int first) {
-      const int piece = (j * WM + wm) * 64 + lane;
-      const int tok = piece / (D / 32) - first, part = piece % (D / 32);
-      if (j * WM + wm >= kVLoads) return;
-      const uint32_t sc = value_scale(x.vs[j]);
-      const bool none = x.vs[j] == 255;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        bf16x2 y[4];
-        fp4_to_bf16x8(none ? 0u : x.v[j][u], sc, y);
-        u32x4 z;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) z[k] = __builtin_bit_cast(uint32_t, y[k]);
-        *reinterpret_cast<u32x4*>(to + tok * S::kVRow + part * 64 + u * 16) = z;
-      }
-    };
-
-    Tile cur, next;
-    int pg[4];
-    pages_of(s0, pg);
-    load(s0, pg, cur);
-    pages_of(s0 + 1, pg);
     char* v_lds = lds + wt * (S::kVTokens * S::kVRow);
     for (int s = s0; s < s1; ++s) {
-      if (s + 1 < s1) {
-        load(s + 1, pg, next);
-        pages_of(s + 2, pg);
-      }
       const int t0 = (s * WT + wt) * S::kTile;
       char* v_tile = v_lds;
+      int pg_now[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) pg_now[u] = pg[u], pg[u] = __builtin_amdgcn_readfirstlane(pg_next[u]);
+      const bool more = s + 1 < s1;
       if constexpr (WM > 1) {
         v_tile += ((s - s0) & 1) * (64 * S::kVRow);
 #pragma unroll
-        for (int j = 0; j < kVMine; ++j) unpack(cur, j, v_tile, 0);
+        for (int j = 0; j < kVMine; ++j) unpack(j, v_tile, 0);
+        if (more) load_values(s + 1, pg);
         __syncthreads();  // and every wave is done with the tile before the last
       }
       if (t0 < need) {
@@ -411,10 +428,16 @@ __global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams 
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < S::kKSteps; ++k) {
-              acc = qp[b].scores(cur.k[u][k], cur.ks[u][k], k, acc);
+              i32x4 codes = kc[u][k];
+              if (D < 128 && quarter >= 2) codes = i32x4{0, 0, 0, 0};
+              acc = qp[b].scores(codes, pg_now[u] < 0 ? 255 : ks[u][k], k, acc);
             }
             sc[b][u] = acc;
           }
+        if (more) {
+          load_keys(s + 1, pg);
+          pages_of(s + 2, pg_next);
+        }
         if (t0 + S::kTile > context) {  // the tile holds new rows or ends
 #pragma unroll
           for (int b = 0; b < MB; ++b) {
@@ -481,7 +504,8 @@ __global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams 
           const char* from = v_tile + (WM == 1 ? 0 : half * 32 * S::kVRow);
           if constexpr (WM == 1) {
 #pragma unroll
-            for (int j = 0; j < kVMine / 2; ++j) unpack(cur, half * (kVMine / 2) + j, v_tile, half * 32);
+            for (int j = 0; j < kVMine / 2; ++j) unpack(half * (kVMine / 2) + j, v_tile, half * 32);
+            if (half == 1 && more) load_values(s + 1, pg);
             wave_lds_sync();
           }
           bf16x8 w8[MB][S::kP];
@@ -513,11 +537,10 @@ __global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams 
           if constexpr (WM == 1) wave_lds_sync();
         }
       }
-      if (s + 1 < s1) cur = next;
     }
 
     // ---- join the waves, and out
-    const bool whole = s0 == 0 && s1 == r.steps;
+    const bool whole = pos == tile_at && stop == tile_end;
     const int slot = 2 * w + (pos == begin ? 0 : 1);
     __syncthreads();  // values in LDS have been read
 #pragma unroll
@@ -569,55 +592,94 @@ __global__ __launch_bounds__(S::kThreads) void kv_attention_kernel(KvAttnParams 
       __syncthreads();
     }
     // the first workgroup whose piece begins inside the tile says where its parts are
-    if (tid == 0 && pos == begin && s0 > 0 && begin - per <= item_at) {
-      const int last = (int)((item_at + r.steps - 1) / per);
-      p.joins[w] = AttnJoin{q, head, m0, min(S::kRows, rows_m - m0), 2 * (w - 1) + (begin - per == item_at ? 0 : 1), last};
-    }
-    pos = item_at + s1;
+    if (tid == 0 && pos == begin && begin > tile_at && begin - per <= tile_at)
+      p.joins[w] = AttnJoin{q, head, m0, min(S::kRows, rows_m - m0), 2 * (w - 1) + (begin - per == tile_at ? 0 : 1),
+                            (int)((tile_end - 1) / per)};
+    pos = stop;
   }
 }
 
-// Joins the parts of a tile that more than one workgroup worked on: block
-// (w, y) rows y, y + gridDim.y, ... of the tile that joins[w] names.  Thread
-// groups of D / 4 lanes take its parts in turn.
-constexpr int kJoinThreads = 256;
+// Joins the parts of the tiles that more than one workgroup worked on.  A unit
+// is four rows of the tile that joins[w] names (most name none): a block looks at
+// 64 units at once and takes those it finds one by one.  A wave has a row; where
+// a tile has many parts, every wave takes a part in four of each row instead.
+constexpr int kJoinThreads = 256, kJoinBlocks = 2048, kJoinMost = 16;
 template <typename TE, int D>
-__global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(KvAttnParams p, int rows) {
-  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
-  __shared__ f32x4 o_lds[kGroups][kLanes];
-  __shared__ float l_lds[kGroups];
-  const int w = blockIdx.x;
-  const AttnJoin j = p.joins[w];
-  if (j.q < 0) return;
-  const int grp = threadIdx.x / kLanes, at = threadIdx.x % kLanes;
-  const int count = j.last - w + 2;  // parts: the first, then 2 w, 2 (w + 1), ...
-  for (int row = blockIdx.y; row < j.rows; row += gridDim.y) {
-    float top = kNegInf;
-    for (int x = 0; x < count; ++x) {
-      const int slot = x ? 2 * (w + x - 1) : j.first;
-      top = fmaxf(top, p.stats[(size_t)slot * rows + row].m);
-    }
-    float l = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int x = grp; x < count; x += kGroups) {
-      const int slot = x ? 2 * (w + x - 1) : j.first;
-      const AttnStat st = p.stats[(size_t)slot * rows + row];
-      const float keep = top == kNegInf ? 1.f : exp2_fast(st.m - top);
-      l += st.l * keep;
-      y += *reinterpret_cast<const f32x4*>(p.parts + ((size_t)slot * rows + row) * D + at * 4) * keep;
-    }
-    __syncthreads();
-    o_lds[grp][at] = y;
-    if (at == 0) l_lds[grp] = l;
-    __syncthreads();
-    if (threadIdx.x < D / 8) {
-      float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-      for (int x = 0; x < kGroups; ++x) {
-        sum += l_lds[x];
+__global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(KvAttnParams p, int rows_shift, int units) {
+  constexpr int kWaves = kJoinThreads / 64, kPer = D / 64;
+  typedef float vec __attribute__((ext_vector_type(kPer)));
+  __shared__ __align__(16) float o_lds[kWaves][D];
+  __shared__ float m_lds[kWaves], l_lds[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = 1 << rows_shift;
+  for (int u0 = blockIdx.x; u0 < units; u0 += 64 * gridDim.x) {
+    const int mine = u0 + lane * (int)gridDim.x;
+    AttnJoin found = {-1, 0, 0, 0, 0, 0};
+    if (mine < units) found = p.joins[mine >> (rows_shift - 2)];
+    const bool on = found.q >= 0 && (mine & (rows / 4 - 1)) * 4 < found.rows;
+    for (uint64_t left = __ballot(on); left; left &= left - 1) {
+      const int at = __builtin_ctzll(left), unit = u0 + at * (int)gridDim.x, w = unit >> (rows_shift - 2);
+      const int first = lane_i32(found.first, at), count = lane_i32(found.last, at) - w + 2;
+      const int valid = lane_i32(found.rows, at), q = lane_i32(found.q, at), head = lane_i32(found.head, at);
+      const int row0 = (unit & (rows / 4 - 1)) * 4, m0 = lane_i32(found.m0, at);
+      const bool split = count > kJoinMost;
+      for (int r = split ? 0 : wave; r < 4; r += split ? 1 : 4) {
+        const int row = row0 + r;
+        if (row >= valid) break;
+        // parts: the first, then 2 w, 2 (w + 1), ...
+        auto slot = [&](int x) { return (size_t)(x ? 2 * (w + x - 1) : first) * rows + row; };
+        float top = kNegInf, l = 0.f;
+        vec y;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) z[k] += o_lds[x][threadIdx.x * 2 + k / 4][k % 4];
+        for (int k = 0; k < kPer; ++k) y[k] = 0.f;
+        const int begin = split ? wave : 0, by = split ? kWaves : 1;
+        for (int x0 = begin; x0 < count; x0 += kJoinMost * by) {
+          vec part[kJoinMost];
+#pragma unroll
+          for (int x = 0; x < kJoinMost; ++x)
+            if (x0 + x * by < count) part[x] = *reinterpret_cast<const vec*>(p.parts + slot(x0 + x * by) * D + lane * kPer);
+          AttnStat st = {kNegInf, 0.f};
+          if (lane < kJoinMost && x0 + lane * by < count) st = p.stats[slot(x0 + lane * by)];
+          const float high = fmaxf(top, row_max(st.m));  // lanes 0..15
+          const float top_new = lane_f32(high, 0);
+          const float old = top == top_new ? 1.f : exp2_fast(top - top_new);
+          const float keep = top_new == kNegInf ? 1.f : exp2_fast(st.m - top_new);
+          top = top_new;
+          l = l * old + st.l * keep;
+          y *= old;
+#pragma unroll
+          for (int x = 0; x < kJoinMost; ++x)
+            if (x0 + x * by < count) y += part[x] * lane_f32(keep, x);
+        }
+        l = wave_sum(lane < kJoinMost ? l : 0.f);
+        *reinterpret_cast<vec*>(&o_lds[wave][lane * kPer]) = y;
+        if (split) {
+          if (lane == 0) m_lds[wave] = top, l_lds[wave] = l;
+          __syncthreads();
+          if (threadIdx.x < D / 8) {
+            float high = kNegInf, sum = 0.f, z[8];
+            for (int x = 0; x < kWaves; ++x) high = fmaxf(high, m_lds[x]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[k] = 0.f;
+            for (int x = 0; x < kWaves; ++x) {
+              const float keep = high == kNegInf ? 1.f : exp2_fast(m_lds[x] - high);
+              sum += l_lds[x] * keep;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) z[k] += o_lds[x][threadIdx.x * 8 + k] * keep;
+            }
+            attn_out<TE, D>(p, q, head, m0 + row, threadIdx.x * 8, high, sum, z);
+          }
+          __syncthreads();
+        } else {
+          wave_lds_sync();
+          if (lane < D / 8) {
+            float z[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[k] = o_lds[wave][lane * 8 + k];
+            attn_out<TE, D>(p, q, head, m0 + row, lane * 8, top, l, z);
+          }
+          wave_lds_sync();
+        }
       }
-      attn_out<TE, D>(p, j.q, j.head, j.m0 + row, threadIdx.x * 8, top, sum, z);
     }
   }
 }

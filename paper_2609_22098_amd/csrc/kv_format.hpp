@@ -144,7 +144,7 @@ struct KvAttnParams {
   float scale_log2;  // scale * log2(e): scores in base-2 units
   void* out;
   float* lse;
-  int min_steps;   // of a workgroup
+  int min_tokens;  // of a workgroup's piece
   float* parts;    // [2 * workgroups][rows of a tile][D]
   AttnStat* stats; // [2 * workgroups][rows of a tile]
   AttnJoin* joins; // [workgroups]
