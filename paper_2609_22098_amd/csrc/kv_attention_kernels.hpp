@@ -35,6 +35,7 @@ namespace ts {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // A tile of 16 * MB * WM rows; WT waves take token tiles in turn, WM waves share
 // one of them.
@@ -214,7 +215,8 @@ __device__ __forceinline__ void attn_out(const KvAttnParams& p, int q, int head,
 }
 
 template <typename S>
-__global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel(KvAttnParams p) {
+__global__ __launch_bounds__(S::kThreads, S::kResident) __attribute__((amdgpu_waves_per_eu(S::kResident, S::kResident)))
+void kv_attention_kernel(KvAttnParams p) {
   constexpr int D = S::D, MB = S::MB, WM = S::WM, WT = S::WT;
   using TE = typename S::TE;
   __shared__ __align__(16) char lds[S::kLds];
@@ -312,14 +314,20 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
     int ks[4][S::kKSteps];
     u32x4 vc[kVMine];         // values
     uint32_t vs[kVMine];
-    // The pages of a tile's runs of 16 tokens, -1 where there is none.
-    auto pages_of = [&](int step, int (&pg)[4]) {
-      const int t0 = (step * WT + wt) * S::kTile;
+    // The table's entries of a tile's runs of 16 tokens, looked at a step before
+    // they are used (a check next to the load would wait for it), and the pages
+    // they name, -1 where there is none.
+    auto look_up = [&](int step, int (&entry)[4]) {
+      const int b0 = ((step * WT + wt) * S::kTile) >> shift;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) entry[u] = table[min(b0 + (16 * u >> shift), p.max_blocks - 1)];
+    };
+    auto pages_of = [&](int step, const int (&entry)[4], int (&pg)[4]) {
+      const int b0 = ((step * WT + wt) * S::kTile) >> shift;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int blk = (t0 + 16 * u) >> shift;
-        const int page = table[min(blk, p.max_blocks - 1)];
-        pg[u] = blk < p.max_blocks && (uint32_t)page < (uint32_t)p.c.num_pages ? page : -1;
+        const int page = __builtin_amdgcn_readfirstlane(entry[u]);
+        pg[u] = b0 + (16 * u >> shift) < p.max_blocks && (uint32_t)page < (uint32_t)p.c.num_pages ? page : -1;
       }
     };
     // Loads of runs without a page go to page 0 and are set aside: keys get
@@ -381,13 +389,12 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
 
     // Each register is loaded again for the next step as soon as this one is
     // done with it; pages are looked up a step earlier.
-    int pg[4], pg_next[4];
-    pages_of(s0, pg);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) pg[u] = __builtin_amdgcn_readfirstlane(pg[u]);
+    int pg[4], entry[4];
+    look_up(s0, entry);
+    pages_of(s0, entry, pg);
+    look_up(s0 + 1, entry);
     load_keys(s0, pg);
     load_values(s0, pg);
-    pages_of(s0 + 1, pg_next);
 
     // ---- queries
     AttnQuery<S> qp[MB];
@@ -409,7 +416,9 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
       char* v_tile = v_lds;
       int pg_now[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) pg_now[u] = pg[u], pg[u] = __builtin_amdgcn_readfirstlane(pg_next[u]);
+      for (int u = 0; u < 4; ++u) pg_now[u] = pg[u];
+      pages_of(s + 1, entry, pg);
+      look_up(s + 2, entry);
       const bool more = s + 1 < s1;
       if constexpr (WM > 1) {
         v_tile += ((s - s0) & 1) * (64 * S::kVRow);
@@ -418,6 +427,21 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
         if (more) load_values(s + 1, pg);
         __syncthreads();  // and every wave is done with the tile before the last
       }
+      // Values as the products' A operand: group `at` is four blocks of 16 elements
+      // of one half of the tile's tokens.
+      constexpr int kGroups = D / 32;
+      s16x8 va[2][4];
+      auto read_group = [&](int at, int buf) {
+        typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+        const int half = at / (kGroups / 2), d0 = at % (kGroups / 2) * 4;
+        const char* from = v_tile + (WM == 1 ? 0 : half * 32 * S::kVRow) + (4 * quarter + col / 4) * S::kVRow + (col % 4) * 8 + d0 * 32;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + x * 32));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + x * 32 + 16 * S::kVRow));
+          va[buf][x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+      };
       if (t0 < need) {
         // scores
         f32x4 sc[MB][4];
@@ -434,10 +458,8 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
             }
             sc[b][u] = acc;
           }
-        if (more) {
-          load_keys(s + 1, pg);
-          pages_of(s + 2, pg_next);
-        }
+        if (more) load_keys(s + 1, pg);
+        if constexpr (WM > 1) read_group(0, 0);  // arrives under the softmax
         if (t0 + S::kTile > context) {  // the tile holds new rows or ends
 #pragma unroll
           for (int b = 0; b < MB; ++b) {
@@ -452,7 +474,7 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
                 const int first = max(j0, 0), w0 = first >> 5, sh = first & 31;
                 uint32_t word[3];
 #pragma unroll
-                for (int u = 0; u < 3; ++u) word[u] = w0 + u < p.mask_words ? bits[w0 + u] : 0u;
+                for (int u = 0; u < 3; ++u) word[u] = bits[min(w0 + u, p.mask_words - 1)];  // what repeats lies past all rows
                 uint64_t win = (((uint64_t)word[1] << 32) | word[0]) >> sh;
                 if (sh) win |= (uint64_t)word[2] << (64 - sh);
                 if (j0 < 0) win = j0 > -64 ? (win << -j0) | ((1ull << -j0) - 1) : ~0ull;
@@ -498,10 +520,9 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
             }
           l_run[b] += sum;
         }
-        // values
+        // values: four blocks of 16 elements at a time, read while the four before are multiplied
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const char* from = v_tile + (WM == 1 ? 0 : half * 32 * S::kVRow);
           if constexpr (WM == 1) {
 #pragma unroll
             for (int j = 0; j < kVMine / 2; ++j) unpack(half * (kVMine / 2) + j, v_tile, half * 32);
@@ -520,21 +541,28 @@ __global__ __launch_bounds__(S::kThreads, S::kResident) void kv_attention_kernel
                 left -= (float)w8[b][piece][e];
               }
             }
+          if constexpr (WM > 1) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-          for (int d = 0; d < D / 16; ++d) {
-            typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-            const char* a = from + (4 * quarter + col / 4) * S::kVRow + d * 32 + (col % 4) * 8;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a + 16 * S::kVRow));
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          for (int g = 0; g < kGroups / 2; ++g) {
+            const int at = half * (kGroups / 2) + g;
+            if constexpr (WM == 1) {
+              read_group(at, at & 1);
+            } else {
+              if (at + 1 < kGroups) read_group(at + 1, (at + 1) & 1);
+              __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
-            for (int b = 0; b < MB; ++b)
+            for (int x = 0; x < 4; ++x)
 #pragma unroll
-              for (int piece = S::kP - 1; piece >= 0; --piece)
-                o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both), w8[b][piece], o[b][d], 0, 0, 0);
+              for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int piece = S::kP - 1; piece >= 0; --piece)
+                  o[b][4 * g + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[at & 1][x]), w8[b][piece],
+                                                                            o[b][4 * g + x], 0, 0, 0);
+            if constexpr (WM > 1) __builtin_amdgcn_sched_barrier(0);
           }
           if constexpr (WM == 1) wave_lds_sync();
+          else __builtin_amdgcn_s_setprio(0);
         }
       }
     }
