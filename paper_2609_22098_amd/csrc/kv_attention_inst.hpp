@@ -15,17 +15,25 @@ static void launch_attention_shape(const KvAttnParams& p, int groups, hipStream_
                      p, __builtin_ctz(S::kRows), units);
 }
 
+template <int D, bool WHOLE>
+static void launch_attention_pages(const KvAttnParams& p, AttnTile tile, bool bf16, int groups, hipStream_t s) {
+  if (bf16) {
+    if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, __bf16, WHOLE>>(p, groups, s);
+    if (tile == AttnTile::k32) launch_attention_shape<AttnShape<D, 2, 1, 4, __bf16, WHOLE>>(p, groups, s);
+    if (tile == AttnTile::k64) launch_attention_shape<AttnShape<D, 2, 2, 2, __bf16, WHOLE>>(p, groups, s);
+    if (tile == AttnTile::k128) launch_attention_shape<AttnShape<D, 2, 4, 1, __bf16, WHOLE>>(p, groups, s);
+  } else {
+    if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, float, WHOLE>>(p, groups, s);
+    if (tile == AttnTile::k64) launch_attention_shape<AttnShape<D, 1, 4, 1, float, WHOLE>>(p, groups, s);
+  }
+}
+
 template <int D>
 void launch_kv_attention_t(const KvAttnParams& p, AttnTile tile, bool bf16, int groups, hipStream_t s) {
-  if (bf16) {
-    if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, __bf16>>(p, groups, s);
-    if (tile == AttnTile::k32) launch_attention_shape<AttnShape<D, 2, 1, 4, __bf16>>(p, groups, s);
-    if (tile == AttnTile::k64) launch_attention_shape<AttnShape<D, 2, 2, 2, __bf16>>(p, groups, s);
-    if (tile == AttnTile::k128) launch_attention_shape<AttnShape<D, 2, 4, 1, __bf16>>(p, groups, s);
-  } else {
-    if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, float>>(p, groups, s);
-    if (tile == AttnTile::k64) launch_attention_shape<AttnShape<D, 1, 4, 1, float>>(p, groups, s);
-  }
+  if (p.c.page_shift >= 6)
+    launch_attention_pages<D, true>(p, tile, bf16, groups, s);
+  else
+    launch_attention_pages<D, false>(p, tile, bf16, groups, s);
 }
 
 }  // namespace ts

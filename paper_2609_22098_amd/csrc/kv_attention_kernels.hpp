@@ -38,14 +38,16 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // A tile of 16 * MB * WM rows; WT waves take token tiles in turn, WM waves share
-// one of them.
-template <int D_, int MB_, int WM_, int WT_, typename TE_>
+// one of them.  kRuns: pages that a token tile may touch: one where pages hold
+// at least a tile (whose addresses are then one base and fixed steps), else four.
+template <int D_, int MB_, int WM_, int WT_, typename TE_, bool WHOLE_>
 struct AttnShape {
   static constexpr int D = D_, MB = MB_, WM = WM_, WT = WT_;
   using TE = TE_;
   static constexpr bool kF32 = sizeof(TE) == 4;
   static constexpr int kThreads = 64 * WM * WT;
   static constexpr int kTile = 64;               // tokens
+  static constexpr int kRuns = WHOLE_ ? 1 : 4;
   static constexpr int kRows = 16 * MB * WM;     // of a workgroup's tile
   static constexpr int kQ = kF32 ? 3 : 2;        // pieces of a query
   static constexpr int kP = kF32 ? 3 : 1;        // pieces of a weight
@@ -112,10 +114,12 @@ struct AttnQuery<S, false> {
     return fmaxf(__builtin_fabsf(scale_log2) * __uint_as_float((uint32_t)max(e - 7, 1) << 23), 1e-36f);
   }
 
-  __device__ __forceinline__ f32x4 scores(i32x4 codes, int scale, int k, f32x4 acc) const {
+  // Product `i` of kProducts with 128 elements of 16 keys: small ones first.
+  static constexpr int kProducts = 2;
+  __device__ __forceinline__ f32x4 product(int i, i32x4 codes, int scale, int k, f32x4 acc) const {
     const i32x8 a = {codes[0], codes[1], codes[2], codes[3], 0, 0, 0, 0};
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][1], acc, 4, 0, 0, scale, 0, 127 - 4);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][0], acc, 4, 0, 0, scale, 0, 127);
+    return i == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][1], acc, 4, 0, 0, scale, 0, 127 - 4)
+                  : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][0], acc, 4, 0, 0, scale, 0, 127);
   }
 };
 
@@ -144,19 +148,15 @@ struct AttnQuery<S, true> {
     return fmaxf(__builtin_fabsf(scale_log2), 1e-36f);
   }
 
-  __device__ __forceinline__ f32x4 scores(i32x4 codes, int scale, int k, f32x4 acc) const {
+  static constexpr int kProducts = 12;
+  __device__ __forceinline__ f32x4 product(int i, i32x4 codes, int scale, int k, f32x4 acc) const {
+    const int piece = 2 - i / 4, u = i % 4;
+    bf16x2 y[4];
+    fp4_to_bf16x8((uint32_t)codes[u], (uint32_t)scale, y);
+    u32x4 a;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      bf16x2 y[4];
-      fp4_to_bf16x8((uint32_t)codes[u], (uint32_t)scale, y);
-      u32x4 a;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) a[j] = scale == 255 ? 0x7FC07FC0u : __builtin_bit_cast(uint32_t, y[j]);
-#pragma unroll
-      for (int piece = 2; piece >= 0; --piece)  // small ones first
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), w[k][u][piece], acc, 0, 0, 0);
-    }
-    return acc;
+    for (int j = 0; j < 4; ++j) a[j] = scale == 255 ? 0x7FC07FC0u : __builtin_bit_cast(uint32_t, y[j]);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), w[k][u][piece], acc, 0, 0, 0);
   }
 };
 
@@ -302,6 +302,7 @@ void kv_attention_kernel(KvAttnParams p) {
     // last position that a row of the tile sees, and so the last step
     const int i_last = min((m0 + S::kRows - 1) / g_rows, r.rows - 1);
     const int need = p.mask ? all_tokens : context + i_last + 1;
+    const int all_seen = p.mask ? context : context + m0 / g_rows + 1;  // what every row sees
     // the workgroup's steps: both sides of a cut round its place up alike
     const int64_t steps = (need + S::kTile * WT - 1) / (S::kTile * WT);
     const int64_t stop = min(end, tile_end);
@@ -314,58 +315,71 @@ void kv_attention_kernel(KvAttnParams p) {
     int ks[4][S::kKSteps];
     u32x4 vc[kVMine];         // values
     uint32_t vs[kVMine];
-    // The table's entries of a tile's runs of 16 tokens, looked at a step before
+    // The table's entries of a tile's runs of tokens, looked at a step before
     // they are used (a check next to the load would wait for it), and the pages
     // they name, -1 where there is none.
-    auto look_up = [&](int step, int (&entry)[4]) {
+    constexpr int kRuns = S::kRuns;
+    auto look_up = [&](int step, int (&entry)[kRuns]) {
       const int b0 = ((step * WT + wt) * S::kTile) >> shift;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) entry[u] = table[min(b0 + (16 * u >> shift), p.max_blocks - 1)];
+      for (int u = 0; u < kRuns; ++u) entry[u] = table[min(b0 + (16 * u >> shift), p.max_blocks - 1)];
     };
-    auto pages_of = [&](int step, const int (&entry)[4], int (&pg)[4]) {
+    auto pages_of = [&](int step, const int (&entry)[kRuns], int (&pg)[kRuns]) {
       const int b0 = ((step * WT + wt) * S::kTile) >> shift;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kRuns; ++u) {
         const int page = __builtin_amdgcn_readfirstlane(entry[u]);
         pg[u] = b0 + (16 * u >> shift) < p.max_blocks && (uint32_t)page < (uint32_t)p.c.num_pages ? page : -1;
       }
     };
     // Loads of runs without a page go to page 0 and are set aside: keys get
     // scale 255, so that their scores are not-a-number, values read as zero.
-    auto load_keys = [&](int step, const int (&pg)[4]) {
+    auto load_keys = [&](int step, const int (&pg)[kRuns]) {
       const int t0 = (step * WT + wt) * S::kTile;
+      const int part = D >= 128 ? quarter : quarter & 1;
+      const int lane_code = col * (D / 2) + part * 16, lane_scale = col * (D / 32) + part;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const char* blk = kv_block<D>(p.c, max(pg[u], 0), head);
-        const int off = ((t0 + 16 * u) & in_page) + col;
+        const int run = kRuns == 1 ? 0 : u, off = (t0 + 16 * run) & in_page, more_off = kRuns == 1 ? 16 * u : 0;
+        const char* blk = kv_block<D>(p.c, max(pg[run], 0), head);
+        const char* codes = blk + KvBlock<D>::key_codes(off);
+        const char* scales = blk + KvBlock<D>::key_scales(off, shift);
 #pragma unroll
         for (int k = 0; k < S::kKSteps; ++k) {
-          const int part = D >= 128 ? k * 4 + quarter : quarter & 1;
-          kc[u][k] = *reinterpret_cast<const i32x4*>(blk + (uint32_t)(KvBlock<D>::key_codes(off) + part * 16));
-          ks[u][k] = (uint8_t)blk[(uint32_t)(KvBlock<D>::key_scales(off, shift) + part)];
+          kc[u][k] = *reinterpret_cast<const i32x4*>(codes + (uint32_t)lane_code + (more_off * (D / 2) + k * 64));
+          ks[u][k] = *reinterpret_cast<const uint8_t*>(scales + (uint32_t)lane_scale + (more_off * (D / 32) + k * 4));
         }
       }
     };
-    auto load_values = [&](int step, const int (&pg)[4]) {
+    auto load_values = [&](int step, const int (&pg)[kRuns]) {
       const int t0 = (step * WT + wt) * S::kTile;
 #pragma unroll
       for (int j = 0; j < kVMine; ++j) {
-        const int piece = (j * WM + wm) * 64 + lane;  // in the tile's 2 D pieces of 32 elements
-        const int tok = piece / (D / 32), part = piece % (D / 32), off = (t0 + tok) & in_page;
-        // a load covers 512 / (D / 4) tokens: one run of 16, half of one or two
-        int page;
-        if constexpr (D == 64) {
-          const int run = min((j * WM + wm) * 2, 2);
-          page = lane < 32 ? pg[0] : pg[1];
-          if (run) page = lane < 32 ? pg[2] : pg[3];
-        } else {
-          const int run = min((j * WM + wm) * 128 / D, 3);
-          page = run == 0 ? pg[0] : run == 1 ? pg[1] : run == 2 ? pg[2] : pg[3];
-        }
         if (j * WM + wm < kVLoads) {
-          const char* blk = kv_block<D>(p.c, max(page, 0), head);
-          vc[j] = *reinterpret_cast<const u32x4*>(blk + (uint32_t)(KvBlock<D>::value_codes(off, shift) + part * 16));
-          vs[j] = page < 0 ? 255u : (uint8_t)blk[(uint32_t)(KvBlock<D>::value_scales(off, shift) + part)];
+          const int piece = (j * WM + wm) * 64 + lane;  // in the tile's 2 D pieces of 32 elements
+          const int tok = piece / (D / 32), part = piece % (D / 32);
+          if constexpr (kRuns == 1) {
+            const int off = t0 & in_page;
+            const char* blk = kv_block<D>(p.c, max(pg[0], 0), head);
+            vc[j] = *reinterpret_cast<const u32x4*>(blk + KvBlock<D>::value_codes(off, shift) + (uint32_t)(piece * 16));
+            vs[j] = *reinterpret_cast<const uint8_t*>(blk + KvBlock<D>::value_scales(off, shift) + (uint32_t)piece);
+            if (pg[0] < 0) vs[j] = 255;
+          } else {
+            // a load covers 2048 / D tokens: half of a run of 16, one or two
+            int page;
+            if constexpr (D == 64) {
+              page = lane < 32 ? pg[0] : pg[1];
+              if (j * WM + wm) page = lane < 32 ? pg[2] : pg[3];
+            } else {
+              const int run = min((j * WM + wm) * 128 / D, 3);
+              page = run == 0 ? pg[0] : run == 1 ? pg[1] : run == 2 ? pg[2] : pg[3];
+            }
+            const int off = (t0 + tok) & in_page;
+            const char* blk = kv_block<D>(p.c, max(page, 0), head);
+            vc[j] = *reinterpret_cast<const u32x4*>(blk + (uint32_t)(KvBlock<D>::value_codes(off, shift) + part * 16));
+            vs[j] = *reinterpret_cast<const uint8_t*>(blk + (uint32_t)(KvBlock<D>::value_scales(off, shift) + part));
+            if (page < 0) vs[j] = 255;
+          }
         }
       }
     };
@@ -389,12 +403,18 @@ void kv_attention_kernel(KvAttnParams p) {
 
     // Each register is loaded again for the next step as soon as this one is
     // done with it; pages are looked up a step earlier.
-    int pg[4], entry[4];
-    look_up(s0, entry);
-    pages_of(s0, entry, pg);
-    look_up(s0 + 1, entry);
-    load_keys(s0, pg);
-    load_values(s0, pg);
+    // Where waves share the values, they are unpacked a step before they are
+    // used: their loads run a step ahead of the keys'.
+    constexpr int kAhead = WM > 1 ? 1 : 0;
+    int pg[2 + kAhead][kRuns], entry[kRuns];  // pages of step s (while s + 1 is loaded), s + 1, s + 2
+#pragma unroll
+    for (int a = 0; a <= kAhead; ++a) {
+      look_up(s0 + a, entry);
+      pages_of(s0 + a, entry, pg[a]);
+      if (a == 0) load_keys(s0, pg[0]);
+      if (a == 0) load_values(s0, pg[0]);
+    }
+    look_up(s0 + 1 + kAhead, entry);
 
     // ---- queries
     AttnQuery<S> qp[MB];
@@ -411,22 +431,19 @@ void kv_attention_kernel(KvAttnParams p) {
     }
 
     char* v_lds = lds + wt * (S::kVTokens * S::kVRow);
+    if constexpr (WM > 1) {
+#pragma unroll
+      for (int j = 0; j < kVMine; ++j) unpack(j, v_lds, 0);
+      if (s0 + 1 < s1) load_values(s0 + 1, pg[1]);
+      __syncthreads();
+    }
     for (int s = s0; s < s1; ++s) {
       const int t0 = (s * WT + wt) * S::kTile;
-      char* v_tile = v_lds;
-      int pg_now[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) pg_now[u] = pg[u];
-      pages_of(s + 1, entry, pg);
-      look_up(s + 2, entry);
+      const bool live = WT == 1 || t0 < need;  // a step's last tiles may lie past the end
       const bool more = s + 1 < s1;
-      if constexpr (WM > 1) {
-        v_tile += ((s - s0) & 1) * (64 * S::kVRow);
-#pragma unroll
-        for (int j = 0; j < kVMine; ++j) unpack(j, v_tile, 0);
-        if (more) load_values(s + 1, pg);
-        __syncthreads();  // and every wave is done with the tile before the last
-      }
+      char* v_tile = v_lds + (WM > 1 ? ((s - s0) & 1) * (64 * S::kVRow) : 0);
+      pages_of(s + 1 + kAhead, entry, pg[1 + kAhead]);
+      look_up(s + 2 + kAhead, entry);
       // Values as the products' A operand: group `at` is four blocks of 16 elements
       // of one half of the tile's tokens.
       constexpr int kGroups = D / 32;
@@ -442,25 +459,36 @@ void kv_attention_kernel(KvAttnParams p) {
           va[buf][x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         }
       };
-      if (t0 < need) {
-        // scores
-        f32x4 sc[MB][4];
+      f32x4 sc[MB][4];
+      if (live) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int b = 0; b < MB; ++b)
 #pragma unroll
-          for (int b = 0; b < MB; ++b) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+          for (int u = 0; u < 4; ++u) sc[b][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < S::kKSteps; ++k) {
+        for (int k = 0; k < S::kKSteps; ++k)
+#pragma unroll
+          for (int i = 0; i < AttnQuery<S>::kProducts; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
               i32x4 codes = kc[u][k];
               if (D < 128 && quarter >= 2) codes = i32x4{0, 0, 0, 0};
-              acc = qp[b].scores(codes, pg_now[u] < 0 ? 255 : ks[u][k], k, acc);
+#pragma unroll
+              for (int b = 0; b < MB; ++b) sc[b][u] = qp[b].product(i, codes, pg[0][kRuns == 1 ? 0 : u] < 0 ? 255 : ks[u][k], k, sc[b][u]);
             }
-            sc[b][u] = acc;
-          }
-        if (more) load_keys(s + 1, pg);
+      }
+      if (more) load_keys(s + 1, pg[1]);
+      if constexpr (WM > 1) {
+        if (more) {
+          char* v_next = v_lds + (((s - s0) & 1) ^ 1) * (64 * S::kVRow);
+#pragma unroll
+          for (int j = 0; j < kVMine; ++j) unpack(j, v_next, 0);
+          if (s + 2 < s1) load_values(s + 2, pg[1 + kAhead]);
+        }
+      }
+      if (live) {
         if constexpr (WM > 1) read_group(0, 0);  // arrives under the softmax
-        if (t0 + S::kTile > context) {  // the tile holds new rows or ends
+        if (t0 + S::kTile > all_seen) {  // some row does not see all of it
 #pragma unroll
           for (int b = 0; b < MB; ++b) {
             uint64_t sees = 0;
@@ -501,7 +529,9 @@ void kv_attention_kernel(KvAttnParams p) {
           top = fmaxf(top, xor16_f32(top));
           top = fmaxf(top, xor32_f32(top));
           top *= c_row[b];
-          if (__any(top > m_run[b])) {
+          // The maximum that weights are taken against may lag by 2^8, which fp32 sums
+          // and bf16 weights hold as well, so that most steps rescale nothing.
+          if (__any(top > m_run[b] + 8.f)) {
             const float m_new = fmaxf(m_run[b], top);
             const float keep = m_new == kNegInf ? 1.f : exp2_fast(m_run[b] - m_new);
             m_run[b] = m_new;
@@ -526,7 +556,7 @@ void kv_attention_kernel(KvAttnParams p) {
           if constexpr (WM == 1) {
 #pragma unroll
             for (int j = 0; j < kVMine / 2; ++j) unpack(half * (kVMine / 2) + j, v_tile, half * 32);
-            if (half == 1 && more) load_values(s + 1, pg);
+            if (half == 1 && more) load_values(s + 1, pg[1]);
             wave_lds_sync();
           }
           bf16x8 w8[MB][S::kP];
@@ -541,7 +571,6 @@ void kv_attention_kernel(KvAttnParams p) {
                 left -= (float)w8[b][piece][e];
               }
             }
-          if constexpr (WM > 1) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
           for (int g = 0; g < kGroups / 2; ++g) {
             const int at = half * (kGroups / 2) + g;
@@ -562,8 +591,13 @@ void kv_attention_kernel(KvAttnParams p) {
             if constexpr (WM > 1) __builtin_amdgcn_sched_barrier(0);
           }
           if constexpr (WM == 1) wave_lds_sync();
-          else __builtin_amdgcn_s_setprio(0);
         }
+      }
+      if constexpr (WM > 1) __syncthreads();  // the next tile's values are there, this one's are done with
+#pragma unroll
+      for (int u = 0; u < kRuns; ++u) {
+        pg[0][u] = pg[1][u];
+        if constexpr (kAhead) pg[1][u] = pg[2][u];
       }
     }
 
