@@ -77,7 +77,7 @@ AttnPlan attn_plan(const ts_kv_cache* c, int32_t cap, int32_t q_heads, int32_t d
   if (dtype == TS_F32)
     x.tile = rows <= 16 ? AttnTile::k16 : AttnTile::k64;
   else
-    x.tile = rows <= 16 ? AttnTile::k16 : rows <= 32 ? AttnTile::k32 : rows <= 64 ? AttnTile::k64 : AttnTile::k128;
+    x.tile = rows <= 16 ? AttnTile::k16 : rows <= 64 ? AttnTile::k32 : AttnTile::k128;
   x.rows = 16 << (int)x.tile;
   x.groups = cus * (x.tile == AttnTile::k16 && dtype == TS_BF16 ? 3 : 2);
   const size_t parts = (size_t)x.groups * 2 * x.rows;

@@ -20,7 +20,6 @@ static void launch_attention_pages(const KvAttnParams& p, AttnTile tile, bool bf
   if (bf16) {
     if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, __bf16, WHOLE>>(p, groups, s);
     if (tile == AttnTile::k32) launch_attention_shape<AttnShape<D, 2, 1, 4, __bf16, WHOLE>>(p, groups, s);
-    if (tile == AttnTile::k64) launch_attention_shape<AttnShape<D, 2, 2, 2, __bf16, WHOLE>>(p, groups, s);
     if (tile == AttnTile::k128) launch_attention_shape<AttnShape<D, 2, 4, 1, __bf16, WHOLE>>(p, groups, s);
   } else {
     if (tile == AttnTile::k16) launch_attention_shape<AttnShape<D, 1, 1, 4, float, WHOLE>>(p, groups, s);

@@ -53,7 +53,7 @@ struct AttnShape {
   static constexpr int kP = kF32 ? 3 : 1;        // pieces of a weight
   static constexpr int kKSteps = D <= 128 ? 1 : D / 128;
   static constexpr int kVRow = 2 * D + 32;       // bytes of a token in LDS: 4 rows of a transposed read on 32 banks
-  static constexpr int kVTokens = WM == 1 ? 32 : 128;  // a wave's half tile; two whole tiles where waves share
+  static constexpr int kVTokens = WM == 1 ? 32 : 192;  // a wave's half tile; three whole tiles where waves share
   static constexpr int kORow = D + 4;            // floats of a row of results in LDS
   static constexpr int kVBytes = WT * kVTokens * kVRow;
   static constexpr int kOBytes = WT * WM * 16 * kORow * 4;
@@ -190,6 +190,17 @@ struct AttnReq {
     return lo;
   }
 };
+
+// Asks the scheduler for `products` matrix instructions with `others` vector
+// instructions after each, in the straight piece of code that it stands in.
+template <int PRODUCTS, int OTHERS>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x2, OTHERS, 0);
+  }
+}
 
 // Eight elements of a finished row m of (request, kv head), and its log-sum-exp.
 template <typename TE, int D>
@@ -334,12 +345,13 @@ void kv_attention_kernel(KvAttnParams p) {
     };
     // Loads of runs without a page go to page 0 and are set aside: keys get
     // scale 255, so that their scores are not-a-number, values read as zero.
-    auto load_keys = [&](int step, const int (&pg)[kRuns]) {
+    auto load_keys = [&](int step, const int (&pg)[kRuns], int half = -1) {  // 0, 2: of runs 0, 1 or 2, 3 alone
       const int t0 = (step * WT + wt) * S::kTile;
       const int part = D >= 128 ? quarter : quarter & 1;
       const int lane_code = col * (D / 2) + part * 16, lane_scale = col * (D / 32) + part;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
+        if (half >= 0 && (u & 2) != half) continue;
         const int run = kRuns == 1 ? 0 : u, off = (t0 + 16 * run) & in_page, more_off = kRuns == 1 ? 16 * u : 0;
         const char* blk = kv_block<D>(p.c, max(pg[run], 0), head);
         const char* codes = blk + KvBlock<D>::key_codes(off);
@@ -349,6 +361,19 @@ void kv_attention_kernel(KvAttnParams p) {
           kc[u][k] = *reinterpret_cast<const i32x4*>(codes + (uint32_t)lane_code + (more_off * (D / 2) + k * 64));
           ks[u][k] = *reinterpret_cast<const uint8_t*>(scales + (uint32_t)lane_scale + (more_off * (D / 32) + k * 4));
         }
+      }
+    };
+    // the page of the lane's part of load j: a load covers 2048 / D tokens, half of
+    // a run of 16, one or two
+    auto value_page = [&](int j, const int (&pg)[kRuns]) {
+      if constexpr (kRuns == 1) {
+        return pg[0];
+      } else if constexpr (D == 64) {
+        const int page = lane < 32 ? pg[0] : pg[1];
+        return j * WM + wm ? (lane < 32 ? pg[2] : pg[3]) : page;
+      } else {
+        const int run = min((j * WM + wm) * 128 / D, 3);
+        return run == 0 ? pg[0] : run == 1 ? pg[1] : run == 2 ? pg[2] : pg[3];
       }
     };
     auto load_values = [&](int step, const int (&pg)[kRuns]) {
@@ -363,33 +388,23 @@ void kv_attention_kernel(KvAttnParams p) {
             const char* blk = kv_block<D>(p.c, max(pg[0], 0), head);
             vc[j] = *reinterpret_cast<const u32x4*>(blk + KvBlock<D>::value_codes(off, shift) + (uint32_t)(piece * 16));
             vs[j] = *reinterpret_cast<const uint8_t*>(blk + KvBlock<D>::value_scales(off, shift) + (uint32_t)piece);
-            if (pg[0] < 0) vs[j] = 255;
           } else {
-            // a load covers 2048 / D tokens: half of a run of 16, one or two
-            int page;
-            if constexpr (D == 64) {
-              page = lane < 32 ? pg[0] : pg[1];
-              if (j * WM + wm) page = lane < 32 ? pg[2] : pg[3];
-            } else {
-              const int run = min((j * WM + wm) * 128 / D, 3);
-              page = run == 0 ? pg[0] : run == 1 ? pg[1] : run == 2 ? pg[2] : pg[3];
-            }
+            const int page = value_page(j, pg);
             const int off = (t0 + tok) & in_page;
             const char* blk = kv_block<D>(p.c, max(page, 0), head);
             vc[j] = *reinterpret_cast<const u32x4*>(blk + (uint32_t)(KvBlock<D>::value_codes(off, shift) + part * 16));
             vs[j] = *reinterpret_cast<const uint8_t*>(blk + (uint32_t)(KvBlock<D>::value_scales(off, shift) + part));
-            if (page < 0) vs[j] = 255;
           }
         }
       }
     };
     // unpack a load's values into LDS, at the tile's token `tok - first`
-    auto unpack = [&](int j, char* to, int first) {
+    auto unpack = [&](int j, const int (&pg)[kRuns], char* to, int first) {
       const int piece = (j * WM + wm) * 64 + lane;
       const int tok = piece / (D / 32) - first, part = piece % (D / 32);
       if (j * WM + wm >= kVLoads) return;
       const uint32_t sc = value_scale(vs[j]);
-      const bool none = vs[j] == 255;
+      const bool none = vs[j] == 255 || value_page(j, pg) < 0;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         bf16x2 y[4];
@@ -431,173 +446,247 @@ void kv_attention_kernel(KvAttnParams p) {
     }
 
     char* v_lds = lds + wt * (S::kVTokens * S::kVRow);
-    if constexpr (WM > 1) {
+    constexpr int kGroups = D / 64;  // of four blocks of 16 elements
+    // Scores of runs u0... of the keys in registers, on the pages `pg`.
+    auto score = [&](auto& x, int u0, const int (&pg_)[kRuns]) {
+      constexpr int N = sizeof(x[0]) / sizeof(x[0][0]);
 #pragma unroll
-      for (int j = 0; j < kVMine; ++j) unpack(j, v_lds, 0);
-      if (s0 + 1 < s1) load_values(s0 + 1, pg[1]);
-      __syncthreads();
-    }
-    for (int s = s0; s < s1; ++s) {
-      const int t0 = (s * WT + wt) * S::kTile;
-      const bool live = WT == 1 || t0 < need;  // a step's last tiles may lie past the end
-      const bool more = s + 1 < s1;
-      char* v_tile = v_lds + (WM > 1 ? ((s - s0) & 1) * (64 * S::kVRow) : 0);
-      pages_of(s + 1 + kAhead, entry, pg[1 + kAhead]);
-      look_up(s + 2 + kAhead, entry);
-      // Values as the products' A operand: group `at` is four blocks of 16 elements
-      // of one half of the tile's tokens.
-      constexpr int kGroups = D / 32;
-      s16x8 va[2][4];
-      auto read_group = [&](int at, int buf) {
-        typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-        const int half = at / (kGroups / 2), d0 = at % (kGroups / 2) * 4;
-        const char* from = v_tile + (WM == 1 ? 0 : half * 32 * S::kVRow) + (4 * quarter + col / 4) * S::kVRow + (col % 4) * 8 + d0 * 32;
+      for (int b = 0; b < MB; ++b)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + x * 32));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + x * 32 + 16 * S::kVRow));
-          va[buf][x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int u = 0; u < N; ++u) x[b][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < S::kKSteps; ++k)
+#pragma unroll
+        for (int i = 0; i < AttnQuery<S>::kProducts; ++i)
+#pragma unroll
+          for (int u = 0; u < N; ++u) {
+            i32x4 codes = kc[u0 + u][k];
+            if (D < 128 && quarter >= 2) codes = i32x4{0, 0, 0, 0};
+            const int scale = pg_[kRuns == 1 ? 0 : u0 + u] < 0 ? 255 : ks[u0 + u][k];
+#pragma unroll
+            for (int b = 0; b < MB; ++b) x[b][u] = qp[b].product(i, codes, scale, k, x[b][u]);
+          }
+    };
+    // -inf for what a row does not see, of runs u0... of the tile at t0.
+    auto hide = [&](auto& x, int u0, int t0) {
+      constexpr int N = sizeof(x[0]) / sizeof(x[0][0]);
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        uint64_t sees = 0;
+        const int i = row_i[b], j0 = t0 - context;
+        if (i >= 0) {
+          if (!p.mask) {
+            const int cnt = min(max(i + 1 - j0, 0), 64);
+            sees = cnt == 64 ? ~0ull : (1ull << cnt) - 1;
+          } else if (t0 < all_tokens) {
+            const uint32_t* bits = p.mask + ((size_t)q * p.cap + i) * p.mask_words;
+            const int first = max(j0, 0), w0 = first >> 5, sh = first & 31;
+            uint32_t word[3];
+#pragma unroll
+            for (int u = 0; u < 3; ++u) word[u] = bits[min(w0 + u, p.mask_words - 1)];  // what repeats lies past all rows
+            uint64_t win = (((uint64_t)word[1] << 32) | word[0]) >> sh;
+            if (sh) win |= (uint64_t)word[2] << (64 - sh);
+            if (j0 < 0) win = j0 > -64 ? (win << -j0) | ((1ull << -j0) - 1) : ~0ull;
+            const int cnt = min(all_tokens - t0, 64);
+            sees = cnt >= 64 ? win : win & ((1ull << cnt) - 1);
+          }
         }
-      };
-      f32x4 sc[MB][4];
-      if (live) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          const uint32_t four = (uint32_t)(sees >> (16 * (u0 + u) + 4 * quarter)) & 15u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[b][u][e] = four >> e & 1 ? x[b][u][e] : kNegInf;
+        }
+      }
+    };
+    auto highest = [&](const auto& x, float (&top)[MB]) {
+      constexpr int N = sizeof(x[0]) / sizeof(x[0][0]);
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        top[b] = kNegInf;
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top[b] = fmaxf(top[b], x[b][u][e]);
+        top[b] = fmaxf(top[b], xor16_f32(top[b]));
+        top[b] = fmaxf(top[b], xor32_f32(top[b])) * c_row[b];
+      }
+    };
+    // The maximum that weights are taken against may lag by 2^8, which fp32 sums
+    // and bf16 weights hold as well, so that most steps rescale nothing.
+    auto rescale = [&](const float (&top)[MB]) {
+      bool rises = false;
+#pragma unroll
+      for (int b = 0; b < MB; ++b) rises |= top[b] > m_run[b] + 8.f;
+      if (__any(rises))
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+          const float m_new = fmaxf(m_run[b], top[b]);
+          const float keep = m_new == kNegInf ? 1.f : exp2_fast(m_run[b] - m_new);
+          m_run[b] = m_new;
+          l_run[b] *= keep;
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) o[b][d] *= keep;
+        }
+    };
+    // Weights of two runs as the products' B operand, and their sum.
+    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP]) {
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        const float sub = m_run[b] == kNegInf ? 0.f : m_run[b];
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float left = exp2_fast(__builtin_fmaf(x[b][u0 + e / 4][e % 4], c_row[b], -sub));
+          sum += left;
+#pragma unroll
+          for (int piece = 0; piece < S::kP; ++piece) {
+            w8[b][piece][e] = (__bf16)left;
+            left -= (float)w8[b][piece][e];
+          }
+        }
+        l_run[b] += sum;
+        // computed here, beside the products, and not where they are used
+#pragma unroll
+        for (int piece = 0; piece < S::kP; ++piece) {
+          u32x4 bits = __builtin_bit_cast(u32x4, w8[b][piece]);
+          asm volatile("" : "+v"(bits));
+          w8[b][piece] = __builtin_bit_cast(bf16x8, bits);
+        }
+      }
+    };
+    // Values of a half tile at `from` as the products' A operand, and the products.
+    s16x8 va[2][4];
+    auto read_group = [&](const char* from, int g) {
+      typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+      const char* at = from + (4 * quarter + col / 4) * S::kVRow + (col % 4) * 8 + g * 128;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + x * 32));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + x * 32 + 16 * S::kVRow));
+        va[g & 1][x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    };
+    auto add_group = [&](int g, const bf16x8 (&w8)[MB][S::kP]) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int b = 0; b < MB; ++b)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) sc[b][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int piece = S::kP - 1; piece >= 0; --piece)
+            o[b][4 * g + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[g & 1][x]), w8[b][piece],
+                                                                      o[b][4 * g + x], 0, 0, 0);
+    };
+
+    if constexpr (WM == 1) {
+      // each wave on its own: bound by the bytes that are on their way
+      for (int s = s0; s < s1; ++s) {
+        const int t0 = (s * WT + wt) * S::kTile;
+        const bool more = s + 1 < s1;
+        pages_of(s + 1, entry, pg[1]);
+        look_up(s + 2, entry);
+        if (t0 < need) {
+          f32x4 sc[MB][4];
+          score(sc, 0, pg[0]);
+          if (more) load_keys(s + 1, pg[1]);
+          if (t0 + S::kTile > all_seen) hide(sc, 0, t0);
+          float top[MB];
+          highest(sc, top);
+          rescale(top);
+          bf16x8 w8[2][MB][S::kP];
+          weigh(sc, 0, w8[0]);
+          weigh(sc, 2, w8[1]);
 #pragma unroll
-        for (int k = 0; k < S::kKSteps; ++k)
+          for (int half = 0; half < 2; ++half) {
 #pragma unroll
-          for (int i = 0; i < AttnQuery<S>::kProducts; ++i)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              i32x4 codes = kc[u][k];
-              if (D < 128 && quarter >= 2) codes = i32x4{0, 0, 0, 0};
-#pragma unroll
-              for (int b = 0; b < MB; ++b) sc[b][u] = qp[b].product(i, codes, pg[0][kRuns == 1 ? 0 : u] < 0 ? 255 : ks[u][k], k, sc[b][u]);
-            }
-      }
-      if (more) load_keys(s + 1, pg[1]);
-      if constexpr (WM > 1) {
-        if (more) {
-          char* v_next = v_lds + (((s - s0) & 1) ^ 1) * (64 * S::kVRow);
-#pragma unroll
-          for (int j = 0; j < kVMine; ++j) unpack(j, v_next, 0);
-          if (s + 2 < s1) load_values(s + 2, pg[1 + kAhead]);
-        }
-      }
-      if (live) {
-        if constexpr (WM > 1) read_group(0, 0);  // arrives under the softmax
-        if (t0 + S::kTile > all_seen) {  // some row does not see all of it
-#pragma unroll
-          for (int b = 0; b < MB; ++b) {
-            uint64_t sees = 0;
-            const int i = row_i[b], j0 = t0 - context;
-            if (i >= 0) {
-              if (!p.mask) {
-                const int cnt = min(max(i + 1 - j0, 0), 64);
-                sees = cnt == 64 ? ~0ull : (1ull << cnt) - 1;
-              } else {
-                const uint32_t* bits = p.mask + ((size_t)q * p.cap + i) * p.mask_words;
-                const int first = max(j0, 0), w0 = first >> 5, sh = first & 31;
-                uint32_t word[3];
-#pragma unroll
-                for (int u = 0; u < 3; ++u) word[u] = bits[min(w0 + u, p.mask_words - 1)];  // what repeats lies past all rows
-                uint64_t win = (((uint64_t)word[1] << 32) | word[0]) >> sh;
-                if (sh) win |= (uint64_t)word[2] << (64 - sh);
-                if (j0 < 0) win = j0 > -64 ? (win << -j0) | ((1ull << -j0) - 1) : ~0ull;
-                const int cnt = min(all_tokens - t0, 64);
-                sees = cnt >= 64 ? win : win & ((1ull << cnt) - 1);
-              }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const uint32_t four = (uint32_t)(sees >> (16 * u + 4 * quarter)) & 15u;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) sc[b][u][e] = four >> e & 1 ? sc[b][u][e] : kNegInf;
-            }
-          }
-        }
-        // weights
-#pragma unroll
-        for (int b = 0; b < MB; ++b) {
-          float top = kNegInf;
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[b][u][e]);
-          top = fmaxf(top, xor16_f32(top));
-          top = fmaxf(top, xor32_f32(top));
-          top *= c_row[b];
-          // The maximum that weights are taken against may lag by 2^8, which fp32 sums
-          // and bf16 weights hold as well, so that most steps rescale nothing.
-          if (__any(top > m_run[b] + 8.f)) {
-            const float m_new = fmaxf(m_run[b], top);
-            const float keep = m_new == kNegInf ? 1.f : exp2_fast(m_run[b] - m_new);
-            m_run[b] = m_new;
-            l_run[b] *= keep;
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) o[b][d] *= keep;
-          }
-          const float sub = m_run[b] == kNegInf ? 0.f : m_run[b];
-          float sum = 0.f;
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              sc[b][u][e] = exp2_fast(__builtin_fmaf(sc[b][u][e], c_row[b], -sub));
-              sum += sc[b][u][e];
-            }
-          l_run[b] += sum;
-        }
-        // values: four blocks of 16 elements at a time, read while the four before are multiplied
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if constexpr (WM == 1) {
-#pragma unroll
-            for (int j = 0; j < kVMine / 2; ++j) unpack(half * (kVMine / 2) + j, v_tile, half * 32);
+            for (int j = 0; j < kVMine / 2; ++j) unpack(half * (kVMine / 2) + j, pg[0], v_lds, half * 32);
             if (half == 1 && more) load_values(s + 1, pg[1]);
             wave_lds_sync();
-          }
-          bf16x8 w8[MB][S::kP];
 #pragma unroll
-          for (int b = 0; b < MB; ++b)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float left = sc[b][2 * half + e / 4][e % 4];
-#pragma unroll
-              for (int piece = 0; piece < S::kP; ++piece) {
-                w8[b][piece][e] = (__bf16)left;
-                left -= (float)w8[b][piece][e];
-              }
+            for (int g = 0; g < kGroups; ++g) {
+              read_group(v_lds, g);
+              add_group(g, w8[half]);
             }
-#pragma unroll
-          for (int g = 0; g < kGroups / 2; ++g) {
-            const int at = half * (kGroups / 2) + g;
-            if constexpr (WM == 1) {
-              read_group(at, at & 1);
-            } else {
-              if (at + 1 < kGroups) read_group(at + 1, (at + 1) & 1);
-              __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-              for (int b = 0; b < MB; ++b)
-#pragma unroll
-                for (int piece = S::kP - 1; piece >= 0; --piece)
-                  o[b][4 * g + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[at & 1][x]), w8[b][piece],
-                                                                            o[b][4 * g + x], 0, 0, 0);
-            if constexpr (WM > 1) __builtin_amdgcn_sched_barrier(0);
+            wave_lds_sync();
           }
-          if constexpr (WM == 1) wave_lds_sync();
         }
-      }
-      if constexpr (WM > 1) __syncthreads();  // the next tile's values are there, this one's are done with
 #pragma unroll
-      for (int u = 0; u < kRuns; ++u) {
-        pg[0][u] = pg[1][u];
-        if constexpr (kAhead) pg[1][u] = pg[2][u];
+        for (int u = 0; u < kRuns; ++u) pg[0][u] = pg[1][u];
+      }
+    } else {
+      // Bound by instructions: a wave's products and its softmax alternate by half
+      // tiles so that one runs under the other.  While half h is scored, the half
+      // before it becomes weights; while the weights' products run, the maximum of
+      // the next half is found.  Values lie in a ring of three tiles: the one that
+      // is unpacked, the one at hand and the one whose second half is still due.
+      constexpr int kSlot = 64 * S::kVRow;
+      int cur = 0, before = 0;
+#pragma unroll
+      for (int j = 0; j < kVMine; ++j) unpack(j, pg[0], v_lds, 0);
+      load_values(s0 + 1, pg[1]);
+      f32x4 sc[2][MB][2];
+      bf16x8 w8[2][MB][S::kP];
+#pragma unroll
+      for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int piece = 0; piece < S::kP; ++piece)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
+      score(sc[0], 0, pg[0]);
+      __syncthreads();
+      read_group(v_lds + 32 * S::kVRow, 0);  // multiplied with weights of zero
+      for (int s = s0; s < s1; ++s) {
+        const int t0 = (s * WT + wt) * S::kTile;
+        const bool part = t0 + S::kTile > all_seen;
+        const int next = cur == 2 * kSlot ? 0 : cur + kSlot;
+        pages_of(s + 2, entry, pg[2]);
+        look_up(s + 3, entry);
+        float top[MB];
+        // What is loaded past the last tile lies in some page and is of no use; a
+        // branch around it would keep the products from running beside the rest.
+        // second half of the tile before, first half of this one
+        if (part) hide(sc[0], 0, t0);
+        load_keys(s + 1, pg[1], 0);
+        highest(sc[0], top);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
+          add_group(g, w8[1]);
+        }
+        interleave<MB * S::kP * D / 16, 3>();
+        rescale(top);
+        read_group(v_lds + cur, 0);
+        score(sc[1], 2, pg[0]);
+        weigh(sc[0], 0, w8[0]);
+        interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
+        // first half of this tile, second half's weights, the next tile's scores
+        if (part) hide(sc[1], 2, t0);
+        load_keys(s + 1, pg[1], 2);
+        highest(sc[1], top);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          if (g + 1 < kGroups) read_group(v_lds + cur, g + 1);
+          add_group(g, w8[0]);
+        }
+#pragma unroll
+        for (int j = 0; j < kVMine; ++j) unpack(j, pg[1], v_lds + next, 0);
+        load_values(s + 2, pg[2]);
+        interleave<MB * S::kP * D / 16, 4>();
+        rescale(top);
+        read_group(v_lds + cur + 32 * S::kVRow, 0);
+        score(sc[0], 0, pg[1]);
+        weigh(sc[1], 0, w8[1]);
+        interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
+        __syncthreads();  // the next tile's values are there, those before this one's are done with
+        before = cur;
+        cur = next;
+#pragma unroll
+        for (int u = 0; u < kRuns; ++u) pg[0][u] = pg[1][u], pg[1][u] = pg[2][u];
+      }
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
+        add_group(g, w8[1]);
       }
     }
 
