@@ -302,11 +302,11 @@ void kv_attention_kernel(KvAttnParams p) {
     const int32_t* table = p.table + (size_t)q * p.max_blocks;
 
     // ---- tokens
-    float m_run[MB], l_run[MB];
+    float m_run[MB], m_neg[MB], l_run[MB];  // the maximum, its negative (0 for none), the sum of weights
     f32x4 o[MB][D / 16];
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
-      m_run[b] = kNegInf, l_run[b] = 0.f;
+      m_run[b] = kNegInf, m_neg[b] = 0.f, l_run[b] = 0.f;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -512,8 +512,8 @@ void kv_attention_kernel(KvAttnParams p) {
         top[b] = fmaxf(top[b], xor32_f32(top[b])) * c_row[b];
       }
     };
-    // The maximum that weights are taken against may lag by 2^8, which fp32 sums
-    // and bf16 weights hold as well, so that most steps rescale nothing.
+    // Raises what weights are taken against to the maximum `top`, which it may lag
+    // behind by 2^8, so that most tiles rescale nothing.
     auto rescale = [&](const float (&top)[MB]) {
       bool rises = false;
 #pragma unroll
@@ -524,28 +524,27 @@ void kv_attention_kernel(KvAttnParams p) {
           const float m_new = fmaxf(m_run[b], top[b]);
           const float keep = m_new == kNegInf ? 1.f : exp2_fast(m_run[b] - m_new);
           m_run[b] = m_new;
+          m_neg[b] = m_new == kNegInf ? 0.f : -m_new;
           l_run[b] *= keep;
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) o[b][d] *= keep;
         }
     };
     // Weights of two runs as the products' B operand, and their sum.
-    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP]) {
+    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP], float (&sum)[MB]) {
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
-        const float sub = m_run[b] == kNegInf ? 0.f : m_run[b];
-        float sum = 0.f;
+        sum[b] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float left = exp2_fast(__builtin_fmaf(x[b][u0 + e / 4][e % 4], c_row[b], -sub));
-          sum += left;
+          float left = exp2_fast(__builtin_fmaf(x[b][u0 + e / 4][e % 4], c_row[b], m_neg[b]));
+          sum[b] += left;
 #pragma unroll
           for (int piece = 0; piece < S::kP; ++piece) {
             w8[b][piece][e] = (__bf16)left;
             left -= (float)w8[b][piece][e];
           }
         }
-        l_run[b] += sum;
         // computed here, beside the products, and not where they are used
 #pragma unroll
         for (int piece = 0; piece < S::kP; ++piece) {
@@ -593,19 +592,21 @@ void kv_attention_kernel(KvAttnParams p) {
           float top[MB];
           highest(sc, top);
           rescale(top);
-          bf16x8 w8[2][MB][S::kP];
-          weigh(sc, 0, w8[0]);
-          weigh(sc, 2, w8[1]);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
 #pragma unroll
             for (int j = 0; j < kVMine / 2; ++j) unpack(half * (kVMine / 2) + j, pg[0], v_lds, half * 32);
             if (half == 1 && more) load_values(s + 1, pg[1]);
+            bf16x8 w8[MB][S::kP];
+            float sum[MB];
+            weigh(sc, 2 * half, w8, sum);
+#pragma unroll
+            for (int b = 0; b < MB; ++b) l_run[b] += sum[b];
             wave_lds_sync();
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
               read_group(v_lds, g);
-              add_group(g, w8[half]);
+              add_group(g, w8);
             }
             wave_lds_sync();
           }
@@ -615,78 +616,124 @@ void kv_attention_kernel(KvAttnParams p) {
       }
     } else {
       // Bound by instructions: a wave's products and its softmax alternate by half
-      // tiles so that one runs under the other.  While half h is scored, the half
-      // before it becomes weights; while the weights' products run, the maximum of
-      // the next half is found.  Values lie in a ring of three tiles: the one that
+      // tiles so that one runs under the other: while a half is scored, the half
+      // before it becomes weights, whose products run beside the loads' work.
+      // The maximum is found for the first half and where rows differ in what they
+      // see; elsewhere weights are taken against what there is, and only where a sum
+      // of them passes kMost is the maximum found and the half weighed again.  (Any
+      // reference serves as long as nothing overflows: fp32 sums and bf16 weights
+      // are as exact at 2^12 as at 1.)  Values lie in a ring of three tiles: the one that
       // is unpacked, the one at hand and the one whose second half is still due.
       constexpr int kSlot = 64 * S::kVRow;
       int cur = 0, before = 0;
 #pragma unroll
       for (int j = 0; j < kVMine; ++j) unpack(j, pg[0], v_lds, 0);
       load_values(s0 + 1, pg[1]);
-      f32x4 sc[2][MB][2];
-      bf16x8 w8[2][MB][S::kP];
+      if (m0 + wm * MB * 16 >= rows_m) {
+        // no rows for this wave: it unpacks its share of the values
+        __syncthreads();
+        for (int s = s0; s < s1; ++s) {
+          const int next = cur == 2 * kSlot ? 0 : cur + kSlot;
+          pages_of(s + 2, entry, pg[2]);
+          look_up(s + 3, entry);
 #pragma unroll
-      for (int b = 0; b < MB; ++b)
+          for (int j = 0; j < kVMine; ++j) unpack(j, pg[1], v_lds + next, 0);
+          load_values(s + 2, pg[2]);
+          __syncthreads();
+          cur = next;
 #pragma unroll
-        for (int piece = 0; piece < S::kP; ++piece)
+          for (int u = 0; u < kRuns; ++u) pg[1][u] = pg[2][u];
+        }
+      } else {
+        f32x4 sc[2][MB][2];
+        bf16x8 w8[2][MB][S::kP];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
-      score(sc[0], 0, pg[0]);
-      __syncthreads();
-      read_group(v_lds + 32 * S::kVRow, 0);  // multiplied with weights of zero
-      for (int s = s0; s < s1; ++s) {
-        const int t0 = (s * WT + wt) * S::kTile;
-        const bool part = t0 + S::kTile > all_seen;
-        const int next = cur == 2 * kSlot ? 0 : cur + kSlot;
-        pages_of(s + 2, entry, pg[2]);
-        look_up(s + 3, entry);
-        float top[MB];
-        // What is loaded past the last tile lies in some page and is of no use; a
-        // branch around it would keep the products from running beside the rest.
-        // second half of the tile before, first half of this one
-        if (part) hide(sc[0], 0, t0);
-        load_keys(s + 1, pg[1], 0);
-        highest(sc[0], top);
+        for (int b = 0; b < MB; ++b)
+#pragma unroll
+          for (int piece = 0; piece < S::kP; ++piece)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
+        float sum[MB];
+        constexpr float kMost = 4096.f;
+        auto raise = [&](auto& x, int u0, int t0, bool part) {
+          if (part) hide(x, u0, t0);
+          float top[MB];
+          highest(x, top);
+          rescale(top);
+        };
+        // The products are issued before this point, not behind the branch that follows
+        // (no instruction: nothing waits for their results).
+        auto stay = [&](f32x4 (&x)[MB][2]) {
+#pragma unroll
+          for (int b = 0; b < MB; ++b) asm volatile("" : "+v"(x[b][0]), "+v"(x[b][1]));
+        };
+        auto settle = [&](auto& x, int u0, int t0, bf16x8 (&w)[MB][S::kP]) {
+          bool over = false;
+#pragma unroll
+          for (int b = 0; b < MB; ++b) over |= sum[b] > kMost;
+          if (__any(over)) {
+            raise(x, u0, t0, false);  // hidden already
+            weigh(x, 0, w, sum);
+          }
+#pragma unroll
+          for (int b = 0; b < MB; ++b) l_run[b] += sum[b];
+        };
+        score(sc[0], 0, pg[0]);
+        __syncthreads();
+        read_group(v_lds + 32 * S::kVRow, 0);  // multiplied with weights of zero
+        for (int s = s0; s < s1; ++s) {
+          const int t0 = (s * WT + wt) * S::kTile;
+          const bool part = t0 + S::kTile > all_seen;
+          const int next = cur == 2 * kSlot ? 0 : cur + kSlot;
+          pages_of(s + 2, entry, pg[2]);
+          look_up(s + 3, entry);
+          const bool first = part || s == s0;
+          // What is loaded past the last tile lies in some page and is of no use; a
+          // branch around it would keep the products from running beside the rest.
+          // second half of the tile before, first half's weights, second half's scores
+          load_keys(s + 1, pg[1], 0);
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
+            add_group(g, w8[1]);
+          }
+          interleave<MB * S::kP * D / 16, 2>();
+          if (first) raise(sc[0], 0, t0, part);
+          read_group(v_lds + cur, 0);
+          score(sc[1], 2, pg[0]);
+          weigh(sc[0], 0, w8[0], sum);
+          stay(sc[1]);
+          interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
+          settle(sc[0], 0, t0, w8[0]);
+          // first half of this tile, second half's weights, the next tile's scores
+          load_keys(s + 1, pg[1], 2);
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            if (g + 1 < kGroups) read_group(v_lds + cur, g + 1);
+            add_group(g, w8[0]);
+          }
+#pragma unroll
+          for (int j = 0; j < kVMine; ++j) unpack(j, pg[1], v_lds + next, 0);
+          load_values(s + 2, pg[2]);
+          interleave<MB * S::kP * D / 16, 4>();
+          if (first) raise(sc[1], 2, t0, part);
+          read_group(v_lds + cur + 32 * S::kVRow, 0);
+          score(sc[0], 0, pg[1]);
+          weigh(sc[1], 0, w8[1], sum);
+          stay(sc[0]);
+          interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
+          settle(sc[1], 2, t0, w8[1]);
+          __syncthreads();  // the next tile's values are there, those before this one's are done with
+          before = cur;
+          cur = next;
+#pragma unroll
+          for (int u = 0; u < kRuns; ++u) pg[0][u] = pg[1][u], pg[1][u] = pg[2][u];
+        }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
           if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
           add_group(g, w8[1]);
         }
-        interleave<MB * S::kP * D / 16, 3>();
-        rescale(top);
-        read_group(v_lds + cur, 0);
-        score(sc[1], 2, pg[0]);
-        weigh(sc[0], 0, w8[0]);
-        interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
-        // first half of this tile, second half's weights, the next tile's scores
-        if (part) hide(sc[1], 2, t0);
-        load_keys(s + 1, pg[1], 2);
-        highest(sc[1], top);
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          if (g + 1 < kGroups) read_group(v_lds + cur, g + 1);
-          add_group(g, w8[0]);
-        }
-#pragma unroll
-        for (int j = 0; j < kVMine; ++j) unpack(j, pg[1], v_lds + next, 0);
-        load_values(s + 2, pg[2]);
-        interleave<MB * S::kP * D / 16, 4>();
-        rescale(top);
-        read_group(v_lds + cur + 32 * S::kVRow, 0);
-        score(sc[0], 0, pg[1]);
-        weigh(sc[1], 0, w8[1]);
-        interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
-        __syncthreads();  // the next tile's values are there, those before this one's are done with
-        before = cur;
-        cur = next;
-#pragma unroll
-        for (int u = 0; u < kRuns; ++u) pg[0][u] = pg[1][u], pg[1][u] = pg[2][u];
-      }
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
-        add_group(g, w8[1]);
       }
     }
 
