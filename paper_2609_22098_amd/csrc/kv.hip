@@ -65,7 +65,7 @@ KvView view(const ts_kv_cache* c, int32_t layer) {
 // their partial results lie in the workspace.
 struct AttnPlan {
   AttnTile tile;
-  int rows, groups;
+  int rows, groups, min_tokens;
   size_t stats, joins, bytes;  // offsets after the parts, and all
 };
 
@@ -80,6 +80,7 @@ AttnPlan attn_plan(const ts_kv_cache* c, int32_t cap, int32_t q_heads, int32_t d
     x.tile = rows <= 16 ? AttnTile::k16 : rows <= 64 ? AttnTile::k32 : AttnTile::k128;
   x.rows = 16 << (int)x.tile;
   x.groups = cus * (x.tile == AttnTile::k16 && dtype == TS_BF16 ? 3 : 2);
+  x.min_tokens = x.tile == AttnTile::k16 || x.tile == AttnTile::k32 ? 256 : 128;  // a step of the former
   const size_t parts = (size_t)x.groups * 2 * x.rows;
   x.stats = parts * c->head_dim * sizeof(float);
   x.joins = x.stats + parts * sizeof(AttnStat);
@@ -215,7 +216,7 @@ int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, 
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   const KvAttnParams p = {view(cache, layer), q, q_stride, q_heads, q_heads / cache->heads, R, cap, max_blocks,
-                          ts_tree_mask_words(cap), len, n, table, mask, scale * kLog2e, out, lse, 256,
+                          ts_tree_mask_words(cap), len, n, table, mask, scale * kLog2e, out, lse, plan.min_tokens,
                           reinterpret_cast<float*>(ws), reinterpret_cast<AttnStat*>(ws + plan.stats),
                           reinterpret_cast<AttnJoin*>(ws + plan.joins)};
   const bool bf16 = dtype == TS_BF16;

@@ -72,23 +72,35 @@ template <typename S>
 struct AttnQuery<S, false> {
   i32x8 w[S::kKSteps][2];
 
+  // The lane's elements as they are, and a step that uses them apart from it, so
+  // that other loads can be sent in between.
+  u32x4 raw[S::kKSteps][4];
+  __device__ __forceinline__ void fetch(const __bf16* x, int quarter) {
+#pragma unroll
+    for (int k = 0; k < S::kKSteps; ++k)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int base = k * 128 + (u / 2) * 64;  // the instruction's order of 8-bit elements
+        if (base < S::D) raw[k][u] = *reinterpret_cast<const u32x4*>(x + base + quarter * 16 + u % 2 * 8);
+        else raw[k][u] = u32x4{0, 0, 0, 0};
+      }
+  }
+
   // Returns what a product's score is multiplied by to give base-2 units.
-  __device__ __forceinline__ float load(const __bf16* x, bool there, int quarter, float scale_log2) {
+  __device__ __forceinline__ float convert(float scale_log2) {
     float v[S::kKSteps][32];
     uint32_t top = 0;
 #pragma unroll
     for (int k = 0; k < S::kKSteps; ++k)
 #pragma unroll
-      for (int e = 0; e < 32; e += 8) {
-        const int d = k * 128 + (e / 16) * 64 + quarter * 16 + e % 16;  // the instruction's order of 8-bit elements
-        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (there && d < S::D) load8(x + d, y);
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[k][e + j] = y[j];
-          top = max(top, __float_as_uint(y[j]) & 0x7FFFFFFFu);
+        for (int j = 0; j < 4; ++j) {
+          v[k][8 * u + 2 * j] = __uint_as_float(raw[k][u][j] << 16);
+          v[k][8 * u + 2 * j + 1] = __uint_as_float(raw[k][u][j] & 0xFFFF0000u);
+          top = max(top, raw[k][u][j] & 0x7FFF0000u);
+          top = max(top, (raw[k][u][j] << 16) & 0x7FFF0000u);
         }
-      }
     top = max(top, (uint32_t)xor16_i32((int)top));
     top = max(top, (uint32_t)xor32_i32((int)top));
     const int e = max((int)(top >> 23), 8);  // x * 2^(134 - e) has its largest in [128, 256)
@@ -127,22 +139,26 @@ template <typename S>
 struct AttnQuery<S, true> {
   bf16x8 w[S::kKSteps][4][3];
 
-  __device__ __forceinline__ float load(const float* x, bool there, int quarter, float scale_log2) {
+  f32x4 raw[S::kKSteps][8];
+  __device__ __forceinline__ void fetch(const float* x, int quarter) {
 #pragma unroll
     for (int k = 0; k < S::kKSteps; ++k)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int d = k * 128 + quarter * 32 + u * 8;
-        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (there && d < S::D) load8(x + d, y);
+      for (int u = 0; u < 8; ++u)  // elements of the lanes past a head of 64 meet keys of zero
+        raw[k][u] = *reinterpret_cast<const f32x4*>(x + k * 128 + (S::D < 128 ? quarter & 1 : quarter) * 32 + u * 4);
+  }
+
+  __device__ __forceinline__ float convert(float scale_log2) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float left = scale_log2 < 0.f ? -y[j] : y[j];
+    for (int k = 0; k < S::kKSteps; ++k)
 #pragma unroll
-          for (int piece = 0; piece < 3; ++piece) {
-            w[k][u][piece][j] = (__bf16)left;
-            left -= (float)w[k][u][piece][j];
-          }
+      for (int j = 0; j < 32; ++j) {
+        const float y = raw[k][j / 4][j % 4];
+        float left = scale_log2 < 0.f ? -y : y;
+#pragma unroll
+        for (int piece = 0; piece < 3; ++piece) {
+          w[k][j / 8][piece][j % 8] = (__bf16)left;
+          left -= (float)w[k][j / 8][piece][j % 8];
         }
       }
     return fmaxf(__builtin_fabsf(scale_log2), 1e-36f);
@@ -190,6 +206,12 @@ struct AttnReq {
     return lo;
   }
 };
+
+__device__ __forceinline__ void store4(float* out, f32x4 v) { *reinterpret_cast<f32x4*>(out) = v; }
+__device__ __forceinline__ void store4(__bf16* out, f32x4 v) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<bf16x4*>(out) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+}
 
 // Asks the scheduler for `products` matrix instructions with `others` vector
 // instructions after each, in the straight piece of code that it stands in.
@@ -422,16 +444,8 @@ void kv_attention_kernel(KvAttnParams p) {
     // used: their loads run a step ahead of the keys'.
     constexpr int kAhead = WM > 1 ? 1 : 0;
     int pg[2 + kAhead][kRuns], entry[kRuns];  // pages of step s (while s + 1 is loaded), s + 1, s + 2
-#pragma unroll
-    for (int a = 0; a <= kAhead; ++a) {
-      look_up(s0 + a, entry);
-      pages_of(s0 + a, entry, pg[a]);
-      if (a == 0) load_keys(s0, pg[0]);
-      if (a == 0) load_values(s0, pg[0]);
-    }
-    look_up(s0 + 1 + kAhead, entry);
-
-    // ---- queries
+    look_up(s0, entry);
+    // queries: those of rows past the last read row 0 and are of no use
     AttnQuery<S> qp[MB];
     float c_row[MB];
     int row_i[MB];
@@ -441,9 +455,19 @@ void kv_attention_kernel(KvAttnParams p) {
       const bool there = m < rows_m;
       const int i = there ? m / g_rows : 0, g = there ? m - i * g_rows : 0;
       row_i[b] = there ? i : -1;
-      const TE* x = static_cast<const TE*>(p.q) + ((int64_t)q * p.cap + i) * p.q_stride + (head * g_rows + g) * D;
-      c_row[b] = qp[b].load(x, there, quarter, p.scale_log2);
+      qp[b].fetch(static_cast<const TE*>(p.q) + ((int64_t)q * p.cap + i) * p.q_stride + (head * g_rows + g) * D, quarter);
     }
+    pages_of(s0, entry, pg[0]);
+    load_keys(s0, pg[0]);
+    load_values(s0, pg[0]);
+    if constexpr (kAhead) {
+      look_up(s0 + 1, entry);
+      pages_of(s0 + 1, entry, pg[1]);
+    }
+    look_up(s0 + 1 + kAhead, entry);
+
+#pragma unroll
+    for (int b = 0; b < MB; ++b) c_row[b] = qp[b].convert(p.scale_log2);
 
     char* v_lds = lds + wt * (S::kVTokens * S::kVRow);
     constexpr int kGroups = D / 64;  // of four blocks of 16 elements
@@ -740,54 +764,77 @@ void kv_attention_kernel(KvAttnParams p) {
     // ---- join the waves, and out
     const bool whole = pos == tile_at && stop == tile_end;
     const int slot = 2 * w + (pos == begin ? 0 : 1);
-    __syncthreads();  // values in LDS have been read
+    if constexpr (WT == 1) {
+      // a wave has all of its rows: four elements a lane
 #pragma unroll
-    for (int b = 0; b < MB; ++b) {
-      l_run[b] = cross_row_sum(l_run[b]);
-      if (quarter == 0) {
-        m_lds[wt][(wm * MB + b) * 16 + col] = m_run[b];
-        l_lds[wt][(wm * MB + b) * 16 + col] = l_run[b];
-      }
-    }
-    __syncthreads();
-    float* o_lds = reinterpret_cast<float*>(lds);
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-      const int mine_row = (wm * MB + b) * 16 + col;
-      float top = kNegInf;
-#pragma unroll
-      for (int u = 0; u < WT; ++u) top = fmaxf(top, m_lds[u][mine_row]);
-      const float keep = top == kNegInf ? 1.f : exp2_fast(m_run[b] - top);
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d)
-        *reinterpret_cast<f32x4*>(o_lds + ((wt * WM + wm) * 16 + col) * S::kORow + d * 16 + quarter * 4) = o[b][d] * keep;
-      __syncthreads();
-      for (int x = tid; x < WM * 16 * (D / 8); x += S::kThreads) {
-        const int row = x / (D / 8), d = x % (D / 8) * 8;  // row: of the waves' blocks b
-        const int m_in = ((row / 16) * MB + b) * 16 + row % 16, m = m0 + m_in;
-        if (m >= rows_m) continue;
-        float top2 = kNegInf;
-#pragma unroll
-        for (int u = 0; u < WT; ++u) top2 = fmaxf(top2, m_lds[u][m_in]);
-        float l = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int u = 0; u < WT; ++u) {
-          l += l_lds[u][m_in] * (top2 == kNegInf ? 1.f : exp2_fast(m_lds[u][m_in] - top2));
-          const float* z = o_lds + (u * WM * 16 + row) * S::kORow + d;
-          const f32x4 z0 = *reinterpret_cast<const f32x4*>(z), z1 = *reinterpret_cast<const f32x4*>(z + 4);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) y[k] += z0[k], y[k + 4] += z1[k];
-        }
+      for (int b = 0; b < MB; ++b) {
+        const float l = cross_row_sum(l_run[b]);
+        const int m_in = (wm * MB + b) * 16 + col;
+        if (row_i[b] < 0) continue;
         if (whole) {
-          attn_out<TE, D>(p, q, head, m, d, top2, l, y);
+          const int64_t row = ((int64_t)q * p.cap + row_i[b]) * p.q_heads + head * g_rows + (m0 + m_in - row_i[b] * g_rows);
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) store4(static_cast<TE*>(p.out) + row * D + d * 16 + quarter * 4, o[b][d] * inv);
+          if (p.lse && quarter == 0) p.lse[row] = l == 0.f ? kNegInf : (m_run[b] + __builtin_amdgcn_logf(l)) * kLn2;
         } else {
-          float* part = p.parts + ((size_t)slot * S::kRows + m_in) * D + d;
-          *reinterpret_cast<f32x4*>(part) = f32x4{y[0], y[1], y[2], y[3]};
-          *reinterpret_cast<f32x4*>(part + 4) = f32x4{y[4], y[5], y[6], y[7]};
-          if (d == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{top2, l};
+          float* part = p.parts + ((size_t)slot * S::kRows + m_in) * D + quarter * 4;
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(part + d * 16) = o[b][d];
+          if (quarter == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{m_run[b], l};
+        }
+      }
+      __syncthreads();  // values in LDS have been read
+    } else {
+      __syncthreads();  // values in LDS have been read
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        l_run[b] = cross_row_sum(l_run[b]);
+        if (quarter == 0) {
+          m_lds[wt][(wm * MB + b) * 16 + col] = m_run[b];
+          l_lds[wt][(wm * MB + b) * 16 + col] = l_run[b];
         }
       }
       __syncthreads();
+      float* o_lds = reinterpret_cast<float*>(lds);
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        const int mine_row = (wm * MB + b) * 16 + col;
+        float top = kNegInf;
+#pragma unroll
+        for (int u = 0; u < WT; ++u) top = fmaxf(top, m_lds[u][mine_row]);
+        const float keep = top == kNegInf ? 1.f : exp2_fast(m_run[b] - top);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+          *reinterpret_cast<f32x4*>(o_lds + ((wt * WM + wm) * 16 + col) * S::kORow + d * 16 + quarter * 4) = o[b][d] * keep;
+        __syncthreads();
+        for (int x = tid; x < WM * 16 * (D / 8); x += S::kThreads) {
+          const int row = x / (D / 8), d = x % (D / 8) * 8;  // row: of the waves' blocks b
+          const int m_in = ((row / 16) * MB + b) * 16 + row % 16, m = m0 + m_in;
+          if (m >= rows_m) continue;
+          float top2 = kNegInf;
+#pragma unroll
+          for (int u = 0; u < WT; ++u) top2 = fmaxf(top2, m_lds[u][m_in]);
+          float l = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int u = 0; u < WT; ++u) {
+            l += l_lds[u][m_in] * (top2 == kNegInf ? 1.f : exp2_fast(m_lds[u][m_in] - top2));
+            const float* z = o_lds + (u * WM * 16 + row) * S::kORow + d;
+            const f32x4 z0 = *reinterpret_cast<const f32x4*>(z), z1 = *reinterpret_cast<const f32x4*>(z + 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] += z0[k], y[k + 4] += z1[k];
+          }
+          if (whole) {
+            attn_out<TE, D>(p, q, head, m, d, top2, l, y);
+          } else {
+            float* part = p.parts + ((size_t)slot * S::kRows + m_in) * D + d;
+            *reinterpret_cast<f32x4*>(part) = f32x4{y[0], y[1], y[2], y[3]};
+            *reinterpret_cast<f32x4*>(part + 4) = f32x4{y[4], y[5], y[6], y[7]};
+            if (d == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{top2, l};
+          }
+        }
+        __syncthreads();
+      }
     }
     // the first workgroup whose piece begins inside the tile says where its parts are
     if (tid == 0 && pos == begin && begin > tile_at && begin - per <= tile_at)
@@ -798,85 +845,87 @@ void kv_attention_kernel(KvAttnParams p) {
 }
 
 // Joins the parts of the tiles that more than one workgroup worked on.  A unit
-// is four rows of the tile that joins[w] names (most name none): a block looks at
-// 64 units at once and takes those it finds one by one.  A wave has a row; where
-// a tile has many parts, every wave takes a part in four of each row instead.
-constexpr int kJoinThreads = 256, kJoinBlocks = 2048, kJoinMost = 16;
-template <typename TE, int D>
-__global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(KvAttnParams p, int rows_shift, int units) {
-  constexpr int kWaves = kJoinThreads / 64, kPer = D / 64;
-  typedef float vec __attribute__((ext_vector_type(kPer)));
-  __shared__ __align__(16) float o_lds[kWaves][D];
-  __shared__ float m_lds[kWaves], l_lds[kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = 1 << rows_shift;
+// is ROWS rows of the tile that joins[w] names (most name none): a block looks at
+// 64 units at once and takes those it finds one by one.  D / 4 lanes hold a row
+// and go through its parts with a running maximum; where a block has more
+// threads than that, groups of them take parts in turn (small tiles are cut into
+// many) and are joined in LDS.
+template <typename TE, int D, int THREADS, int ROWS>
+__global__ __launch_bounds__(THREADS) void kv_join_kernel(KvAttnParams p, int rows_shift, int pieces) {
+  constexpr int kLanes = D / 4, kGroups = THREADS / (ROWS * kLanes), kBatch = 8, kUnit = __builtin_ctz(ROWS);
+  __shared__ __align__(16) f32x4 o_lds[kGroups > 1 ? kGroups : 1][ROWS][kLanes];
+  __shared__ AttnStat s_lds[kGroups][ROWS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int row = tid / kLanes % ROWS, grp = tid / kLanes / ROWS, at = tid % kLanes;
+  // the pieces' first rows, then their next ones, ..., each turned a little, so
+  // that few tiles of many rows spread over the blocks
+  const int units = pieces << (rows_shift - kUnit);
+  auto piece_of = [&](int unit) { return (unit + unit / pieces * 61) % pieces; };
   for (int u0 = blockIdx.x; u0 < units; u0 += 64 * gridDim.x) {
     const int mine = u0 + lane * (int)gridDim.x;
     AttnJoin found = {-1, 0, 0, 0, 0, 0};
-    if (mine < units) found = p.joins[mine >> (rows_shift - 2)];
-    const bool on = found.q >= 0 && (mine & (rows / 4 - 1)) * 4 < found.rows;
+    if (mine < units) found = p.joins[piece_of(mine)];
+    const bool on = found.q >= 0 && (mine / pieces << kUnit) < found.rows;
     for (uint64_t left = __ballot(on); left; left &= left - 1) {
-      const int at = __builtin_ctzll(left), unit = u0 + at * (int)gridDim.x, w = unit >> (rows_shift - 2);
-      const int first = lane_i32(found.first, at), count = lane_i32(found.last, at) - w + 2;
-      const int valid = lane_i32(found.rows, at), q = lane_i32(found.q, at), head = lane_i32(found.head, at);
-      const int row0 = (unit & (rows / 4 - 1)) * 4, m0 = lane_i32(found.m0, at);
-      const bool split = count > kJoinMost;
-      for (int r = split ? 0 : wave; r < 4; r += split ? 1 : 4) {
-        const int row = row0 + r;
-        if (row >= valid) break;
-        // parts: the first, then 2 w, 2 (w + 1), ...
-        auto slot = [&](int x) { return (size_t)(x ? 2 * (w + x - 1) : first) * rows + row; };
-        float top = kNegInf, l = 0.f;
-        vec y;
+      const int bit = __builtin_ctzll(left), unit = u0 + bit * (int)gridDim.x, w = piece_of(unit);
+      const int first = lane_i32(found.first, bit), count = lane_i32(found.last, bit) - w + 2;
+      const int row_in = (unit / pieces << kUnit) + row;
+      // the row of part x: the first, then those of slots 2 w, 2 (w + 1), ...
+      auto place = [&](int x) { return ((size_t)(x ? 2 * (w + x - 1) : first) << rows_shift) + row_in; };
+      float top = kNegInf, l = 0.f;
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+      for (int x0 = grp; x0 < count; x0 += kBatch * kGroups) {
+        f32x4 part[kBatch];
+        AttnStat st[kBatch];
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) y[k] = 0.f;
-        const int begin = split ? wave : 0, by = split ? kWaves : 1;
-        for (int x0 = begin; x0 < count; x0 += kJoinMost * by) {
-          vec part[kJoinMost];
-#pragma unroll
-          for (int x = 0; x < kJoinMost; ++x)
-            if (x0 + x * by < count) part[x] = *reinterpret_cast<const vec*>(p.parts + slot(x0 + x * by) * D + lane * kPer);
-          AttnStat st = {kNegInf, 0.f};
-          if (lane < kJoinMost && x0 + lane * by < count) st = p.stats[slot(x0 + lane * by)];
-          const float high = fmaxf(top, row_max(st.m));  // lanes 0..15
-          const float top_new = lane_f32(high, 0);
-          const float old = top == top_new ? 1.f : exp2_fast(top - top_new);
-          const float keep = top_new == kNegInf ? 1.f : exp2_fast(st.m - top_new);
-          top = top_new;
-          l = l * old + st.l * keep;
-          y *= old;
-#pragma unroll
-          for (int x = 0; x < kJoinMost; ++x)
-            if (x0 + x * by < count) y += part[x] * lane_f32(keep, x);
-        }
-        l = wave_sum(lane < kJoinMost ? l : 0.f);
-        *reinterpret_cast<vec*>(&o_lds[wave][lane * kPer]) = y;
-        if (split) {
-          if (lane == 0) m_lds[wave] = top, l_lds[wave] = l;
-          __syncthreads();
-          if (threadIdx.x < D / 8) {
-            float high = kNegInf, sum = 0.f, z[8];
-            for (int x = 0; x < kWaves; ++x) high = fmaxf(high, m_lds[x]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) z[k] = 0.f;
-            for (int x = 0; x < kWaves; ++x) {
-              const float keep = high == kNegInf ? 1.f : exp2_fast(m_lds[x] - high);
-              sum += l_lds[x] * keep;
-#pragma unroll
-              for (int k = 0; k < 8; ++k) z[k] += o_lds[x][threadIdx.x * 8 + k] * keep;
-            }
-            attn_out<TE, D>(p, q, head, m0 + row, threadIdx.x * 8, high, sum, z);
+        for (int b = 0; b < kBatch; ++b)
+          if (x0 + b * kGroups < count) {
+            const size_t from = place(x0 + b * kGroups);
+            part[b] = *reinterpret_cast<const f32x4*>(p.parts + from * D + at * 4);
+            st[b] = p.stats[from];
+          } else {
+            part[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+            st[b] = AttnStat{kNegInf, 0.f};
           }
-          __syncthreads();
-        } else {
-          wave_lds_sync();
-          if (lane < D / 8) {
-            float z[8];
+        float high = top;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) z[k] = o_lds[wave][lane * 8 + k];
-            attn_out<TE, D>(p, q, head, m0 + row, lane * 8, top, l, z);
-          }
-          wave_lds_sync();
+        for (int b = 0; b < kBatch; ++b) high = fmaxf(high, st[b].m);
+        const float sub = high == kNegInf ? 0.f : high, old = exp2_fast(top - sub);
+        l *= old;
+        y *= old;
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const float keep = exp2_fast(st[b].m - sub);
+          l += st[b].l * (st[b].m == kNegInf ? 1.f : keep);  // a row of not-a-numbers has no maximum
+          y += part[b] * (st[b].m == kNegInf ? 1.f : keep);
         }
+        top = high;
+      }
+      if constexpr (kGroups > 1) {
+        __syncthreads();  // the unit before has been read
+        o_lds[grp][row][at] = y;
+        if (at == 0) s_lds[grp][row] = AttnStat{top, l};
+        __syncthreads();
+        if (grp == 0) {
+          float high = kNegInf;
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) high = fmaxf(high, s_lds[g][row].m);
+          l = 0.f, y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            const AttnStat st = s_lds[g][row];
+            const float keep = st.m == kNegInf ? 1.f : exp2_fast(st.m - high);
+            l += st.l * keep;
+            y += o_lds[g][row][at] * keep;
+          }
+          top = high;
+        }
+      }
+      if (grp == 0 && row_in < lane_i32(found.rows, bit)) {
+        const int m = lane_i32(found.m0, bit) + row_in, i = m / p.group;
+        const int64_t out_row = ((int64_t)lane_i32(found.q, bit) * p.cap + i) * p.q_heads + lane_i32(found.head, bit) * p.group + (m - i * p.group);
+        store4(static_cast<TE*>(p.out) + out_row * D + at * 4, y * (l == 0.f ? 0.f : 1.f / l));
+        if (p.lse && at == 0) p.lse[out_row] = l == 0.f ? kNegInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
       }
     }
   }
