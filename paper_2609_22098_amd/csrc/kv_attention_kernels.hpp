@@ -227,11 +227,11 @@ __device__ __forceinline__ void interleave() {
 // Eight elements of a finished row m of (request, kv head), and its log-sum-exp.
 template <typename TE, int D>
 __device__ __forceinline__ void attn_out(const KvAttnParams& p, int q, int head, int m, int d, float top, float l,
-                                         const float (&y)[8]) {
+                                         float r, const float (&y)[8]) {
   const int i = m / p.group, a = head * p.group + (m - i * p.group);
   const int64_t row = ((int64_t)q * p.cap + i) * p.q_heads + a;
   TE* out = static_cast<TE*>(p.out) + row * D + d;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = r == 0.f ? 0.f : 1.f / r;
   if constexpr (sizeof(TE) == 2) {
     bf16x8 z;
 #pragma unroll
@@ -253,7 +253,7 @@ void kv_attention_kernel(KvAttnParams p) {
   constexpr int D = S::D, MB = S::MB, WM = S::WM, WT = S::WT;
   using TE = typename S::TE;
   __shared__ __align__(16) char lds[S::kLds];
-  __shared__ float m_lds[WT][S::kRows], l_lds[WT][S::kRows];
+  __shared__ float m_lds[WT][S::kRows], l_lds[WT][S::kRows], r_lds[WT][S::kRows];
   __shared__ int64_t sum_lds[S::kThreads / 64];
   __shared__ int found;
   __shared__ int64_t found_at;
@@ -324,11 +324,11 @@ void kv_attention_kernel(KvAttnParams p) {
     const int32_t* table = p.table + (size_t)q * p.max_blocks;
 
     // ---- tokens
-    float m_run[MB], m_neg[MB], l_run[MB];  // the maximum, its negative (0 for none), the sum of weights
+    float m_run[MB], m_neg[MB], l_run[MB], r_run[MB];  // the maximum, its negative (0 for none), the sums of weights
     f32x4 o[MB][D / 16];
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
-      m_run[b] = kNegInf, m_neg[b] = 0.f, l_run[b] = 0.f;
+      m_run[b] = kNegInf, m_neg[b] = 0.f, l_run[b] = 0.f, r_run[b] = 0.f;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -550,15 +550,19 @@ void kv_attention_kernel(KvAttnParams p) {
           m_run[b] = m_new;
           m_neg[b] = m_new == kNegInf ? 0.f : -m_new;
           l_run[b] *= keep;
+          r_run[b] *= keep;
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) o[b][d] *= keep;
         }
     };
-    // Weights of two runs as the products' B operand, and their sum.
-    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP], float (&sum)[MB]) {
+    // Weights of two runs as the products' B operand, and their sums: as they are
+    // for the log-sum-exp, and as the products take them, which is what outputs are
+    // divided by, so that the rounding of a row's large weights cancels.
+    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP], float (&sum)[MB], float (&rsum)[MB]) {
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
         sum[b] = 0.f;
+        rsum[b] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float left = exp2_fast(__builtin_fmaf(x[b][u0 + e / 4][e % 4], c_row[b], m_neg[b]));
@@ -575,6 +579,12 @@ void kv_attention_kernel(KvAttnParams p) {
           u32x4 bits = __builtin_bit_cast(u32x4, w8[b][piece]);
           asm volatile("" : "+v"(bits));
           w8[b][piece] = __builtin_bit_cast(bf16x8, bits);
+        }
+        if constexpr (S::kP == 1) {
+          const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+          for (int e = 0; e < 8; e += 2)
+            rsum[b] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w8[b][0][e], w8[b][0][e + 1]}, ones, rsum[b], false);
         }
       }
     };
@@ -622,10 +632,10 @@ void kv_attention_kernel(KvAttnParams p) {
             for (int j = 0; j < kVMine / 2; ++j) unpack(half * (kVMine / 2) + j, pg[0], v_lds, half * 32);
             if (half == 1 && more) load_values(s + 1, pg[1]);
             bf16x8 w8[MB][S::kP];
-            float sum[MB];
-            weigh(sc, 2 * half, w8, sum);
+            float sum[MB], rsum[MB];
+            weigh(sc, 2 * half, w8, sum, rsum);
 #pragma unroll
-            for (int b = 0; b < MB; ++b) l_run[b] += sum[b];
+            for (int b = 0; b < MB; ++b) l_run[b] += sum[b], r_run[b] += rsum[b];
             wave_lds_sync();
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
@@ -677,7 +687,7 @@ void kv_attention_kernel(KvAttnParams p) {
           for (int piece = 0; piece < S::kP; ++piece)
 #pragma unroll
             for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
-        float sum[MB];
+        float sum[MB], rsum[MB];
         constexpr float kMost = 4096.f;
         auto raise = [&](auto& x, int u0, int t0, bool part) {
           if (part) hide(x, u0, t0);
@@ -697,10 +707,10 @@ void kv_attention_kernel(KvAttnParams p) {
           for (int b = 0; b < MB; ++b) over |= sum[b] > kMost;
           if (__any(over)) {
             raise(x, u0, t0, false);  // hidden already
-            weigh(x, 0, w, sum);
+            weigh(x, 0, w, sum, rsum);
           }
 #pragma unroll
-          for (int b = 0; b < MB; ++b) l_run[b] += sum[b];
+          for (int b = 0; b < MB; ++b) l_run[b] += sum[b], r_run[b] += rsum[b];
         };
         score(sc[0], 0, pg[0]);
         __syncthreads();
@@ -725,7 +735,7 @@ void kv_attention_kernel(KvAttnParams p) {
           if (first) raise(sc[0], 0, t0, part);
           read_group(v_lds + cur, 0);
           score(sc[1], 2, pg[0]);
-          weigh(sc[0], 0, w8[0], sum);
+          weigh(sc[0], 0, w8[0], sum, rsum);
           stay(sc[1]);
           interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
           settle(sc[0], 0, t0, w8[0]);
@@ -743,7 +753,7 @@ void kv_attention_kernel(KvAttnParams p) {
           if (first) raise(sc[1], 2, t0, part);
           read_group(v_lds + cur + 32 * S::kVRow, 0);
           score(sc[0], 0, pg[1]);
-          weigh(sc[1], 0, w8[1], sum);
+          weigh(sc[1], 0, w8[1], sum, rsum);
           stay(sc[0]);
           interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
           settle(sc[1], 2, t0, w8[1]);
@@ -768,12 +778,12 @@ void kv_attention_kernel(KvAttnParams p) {
       // a wave has all of its rows: four elements a lane
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
-        const float l = cross_row_sum(l_run[b]);
+        const float l = cross_row_sum(l_run[b]), r = S::kP == 1 ? cross_row_sum(r_run[b]) : l;
         const int m_in = (wm * MB + b) * 16 + col;
         if (row_i[b] < 0) continue;
         if (whole) {
           const int64_t row = ((int64_t)q * p.cap + row_i[b]) * p.q_heads + head * g_rows + (m0 + m_in - row_i[b] * g_rows);
-          const float inv = l == 0.f ? 0.f : 1.f / l;
+          const float inv = r == 0.f ? 0.f : 1.f / r;
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) store4(static_cast<TE*>(p.out) + row * D + d * 16 + quarter * 4, o[b][d] * inv);
           if (p.lse && quarter == 0) p.lse[row] = l == 0.f ? kNegInf : (m_run[b] + __builtin_amdgcn_logf(l)) * kLn2;
@@ -781,7 +791,7 @@ void kv_attention_kernel(KvAttnParams p) {
           float* part = p.parts + ((size_t)slot * S::kRows + m_in) * D + quarter * 4;
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(part + d * 16) = o[b][d];
-          if (quarter == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{m_run[b], l};
+          if (quarter == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{m_run[b], l, r, 0.f};
         }
       }
       __syncthreads();  // values in LDS have been read
@@ -790,9 +800,11 @@ void kv_attention_kernel(KvAttnParams p) {
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
         l_run[b] = cross_row_sum(l_run[b]);
+        r_run[b] = S::kP == 1 ? cross_row_sum(r_run[b]) : l_run[b];
         if (quarter == 0) {
           m_lds[wt][(wm * MB + b) * 16 + col] = m_run[b];
           l_lds[wt][(wm * MB + b) * 16 + col] = l_run[b];
+          r_lds[wt][(wm * MB + b) * 16 + col] = r_run[b];
         }
       }
       __syncthreads();
@@ -815,22 +827,24 @@ void kv_attention_kernel(KvAttnParams p) {
           float top2 = kNegInf;
 #pragma unroll
           for (int u = 0; u < WT; ++u) top2 = fmaxf(top2, m_lds[u][m_in]);
-          float l = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+          float l = 0.f, r = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int u = 0; u < WT; ++u) {
-            l += l_lds[u][m_in] * (top2 == kNegInf ? 1.f : exp2_fast(m_lds[u][m_in] - top2));
+            const float keep_u = top2 == kNegInf ? 1.f : exp2_fast(m_lds[u][m_in] - top2);
+            l += l_lds[u][m_in] * keep_u;
+            r += r_lds[u][m_in] * keep_u;
             const float* z = o_lds + (u * WM * 16 + row) * S::kORow + d;
             const f32x4 z0 = *reinterpret_cast<const f32x4*>(z), z1 = *reinterpret_cast<const f32x4*>(z + 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k) y[k] += z0[k], y[k + 4] += z1[k];
           }
           if (whole) {
-            attn_out<TE, D>(p, q, head, m, d, top2, l, y);
+            attn_out<TE, D>(p, q, head, m, d, top2, l, r, y);
           } else {
             float* part = p.parts + ((size_t)slot * S::kRows + m_in) * D + d;
             *reinterpret_cast<f32x4*>(part) = f32x4{y[0], y[1], y[2], y[3]};
             *reinterpret_cast<f32x4*>(part + 4) = f32x4{y[4], y[5], y[6], y[7]};
-            if (d == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{top2, l};
+            if (d == 0) p.stats[(size_t)slot * S::kRows + m_in] = AttnStat{top2, l, r, 0.f};
           }
         }
         __syncthreads();
@@ -872,7 +886,7 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvAttnParams p, int ro
       const int row_in = (unit / pieces << kUnit) + row;
       // the row of part x: the first, then those of slots 2 w, 2 (w + 1), ...
       auto place = [&](int x) { return ((size_t)(x ? 2 * (w + x - 1) : first) << rows_shift) + row_in; };
-      float top = kNegInf, l = 0.f;
+      float top = kNegInf, l = 0.f, r = 0.f;
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
       for (int x0 = grp; x0 < count; x0 += kBatch * kGroups) {
         f32x4 part[kBatch];
@@ -885,37 +899,40 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvAttnParams p, int ro
             st[b] = p.stats[from];
           } else {
             part[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-            st[b] = AttnStat{kNegInf, 0.f};
+            st[b] = AttnStat{kNegInf, 0.f, 0.f, 0.f};
           }
         float high = top;
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) high = fmaxf(high, st[b].m);
         const float sub = high == kNegInf ? 0.f : high, old = exp2_fast(top - sub);
         l *= old;
+        r *= old;
         y *= old;
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const float keep = exp2_fast(st[b].m - sub);
-          l += st[b].l * (st[b].m == kNegInf ? 1.f : keep);  // a row of not-a-numbers has no maximum
-          y += part[b] * (st[b].m == kNegInf ? 1.f : keep);
+          const float keep = st[b].m == kNegInf ? 1.f : exp2_fast(st[b].m - sub);  // a row of not-a-numbers has no maximum
+          l += st[b].l * keep;
+          r += st[b].r * keep;
+          y += part[b] * keep;
         }
         top = high;
       }
       if constexpr (kGroups > 1) {
         __syncthreads();  // the unit before has been read
         o_lds[grp][row][at] = y;
-        if (at == 0) s_lds[grp][row] = AttnStat{top, l};
+        if (at == 0) s_lds[grp][row] = AttnStat{top, l, r, 0.f};
         __syncthreads();
         if (grp == 0) {
           float high = kNegInf;
 #pragma unroll
           for (int g = 0; g < kGroups; ++g) high = fmaxf(high, s_lds[g][row].m);
-          l = 0.f, y = f32x4{0.f, 0.f, 0.f, 0.f};
+          l = 0.f, r = 0.f, y = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int g = 0; g < kGroups; ++g) {
             const AttnStat st = s_lds[g][row];
             const float keep = st.m == kNegInf ? 1.f : exp2_fast(st.m - high);
             l += st.l * keep;
+            r += st.r * keep;
             y += o_lds[g][row][at] * keep;
           }
           top = high;
@@ -924,7 +941,7 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvAttnParams p, int ro
       if (grp == 0 && row_in < lane_i32(found.rows, bit)) {
         const int m = lane_i32(found.m0, bit) + row_in, i = m / p.group;
         const int64_t out_row = ((int64_t)lane_i32(found.q, bit) * p.cap + i) * p.q_heads + lane_i32(found.head, bit) * p.group + (m - i * p.group);
-        store4(static_cast<TE*>(p.out) + out_row * D + at * 4, y * (l == 0.f ? 0.f : 1.f / l));
+        store4(static_cast<TE*>(p.out) + out_row * D + at * 4, y * (r == 0.f ? 0.f : 1.f / r));
         if (p.lse && at == 0) p.lse[out_row] = l == 0.f ? kNegInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
       }
     }

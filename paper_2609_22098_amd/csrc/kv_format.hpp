@@ -123,9 +123,10 @@ struct KvAcceptParams {
 // Row tiles of the attention kernel: rows of a workgroup's tile and its waves (see AttnShape).
 enum class AttnTile : int { k16, k32, k64, k128 };
 
-// A partial result's statistics: running maximum (base-2 units) and sum of weights.
-struct AttnStat {
-  float m, l;
+// A partial result's statistics: what weights are taken against (base-2 units),
+// their sum, and the sum of what the products took of them.
+struct alignas(16) AttnStat {
+  float m, l, r, unused;
 };
 // A row tile whose parts a second kernel joins; q < 0: none.
 struct AttnJoin {
