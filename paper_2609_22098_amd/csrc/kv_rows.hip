@@ -44,7 +44,7 @@ void launch_kv_read(const KvReadParams& p, int head_dim, bool bf16, hipStream_t 
 void launch_kv_accept(const KvAcceptParams& p, int head_dim, hipStream_t s) {
   with_dim(head_dim, [&](auto d) {
     constexpr int D = decltype(d)::value;
-    hipLaunchKernelGGL((kv_accept_kernel<D>), dim3(p.R, p.layers), dim3(kRowThreads), 0, s, p);
+    hipLaunchKernelGGL((kv_accept_kernel<D>), dim3(p.R, p.layers), dim3(kAcceptThreads), 0, s, p);
   });
 }
 

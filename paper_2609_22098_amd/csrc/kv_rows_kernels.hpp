@@ -115,71 +115,82 @@ __global__ __launch_bounds__(kRowThreads) void kv_read_kernel(KvReadParams p) {
   }
 }
 
-// The accepted rows of a request in one layer: a thread owns a word of the
-// rows of one head, reads it of all accepted rows and then writes it, so that no
-// order among the rows matters (a row's new place may be another's old one).
-// A word of a row: D/8 of key codes, then value codes, then D/128 (at least
-// one half) of each scale; scales are moved in pieces of 2 bytes.
+// The accepted rows of a request in one layer.  A thread owns a piece of the
+// rows of one head (16 bytes of codes, or a row's scales), reads it of all accepted
+// rows and then writes it, so that no order among the rows matters (a row's new
+// place may be another's old one).  The path is looked up by a wave, a lane to a
+// node.  Bound by the bytes where there are many requests and layers.
+template <int BYTES>
+struct KvPiece;
+template <>
+struct KvPiece<2> { typedef uint16_t type; };
+template <>
+struct KvPiece<4> { typedef uint32_t type; };
+template <>
+struct KvPiece<8> { typedef uint64_t type; };
+template <>
+struct KvPiece<16> { typedef u32x4 type; };
+
+// Moves a piece of BYTES at offset `at` + off * step of each row's block.
+template <int BYTES, int D>
+__device__ __forceinline__ void kv_move(char* base, const int64_t* src, const int64_t* dst, const int* src_off,
+                                        const int* dst_off, int kept, int at, int step) {
+  typedef typename KvPiece<BYTES>::type T;
+  T w[TS_MAX_D];
+#pragma unroll
+  for (int j = 0; j < TS_MAX_D; ++j)
+    if (j < kept) w[j] = *reinterpret_cast<const T*>(base + src[j] + at + src_off[j] * step);
+#pragma unroll
+  for (int j = 0; j < TS_MAX_D; ++j)
+    if (j < kept) *reinterpret_cast<T*>(base + dst[j] + at + dst_off[j] * step) = w[j];
+}
+
+constexpr int kAcceptThreads = 128;
 template <int D>
-__global__ __launch_bounds__(kRowThreads) void kv_accept_kernel(KvAcceptParams p) {
-  constexpr int kCodeWords = D / 8, kScaleHalves = D / 64;
-  constexpr int kPieces = 2 * kCodeWords + 2 * kScaleHalves;
-  __shared__ int src[TS_MAX_D], dst[TS_MAX_D];
+__global__ __launch_bounds__(kAcceptThreads) void kv_accept_kernel(KvAcceptParams p) {
+  constexpr int kCodes = D / 32, kPieces = 2 * kCodes + 2;  // of a row of one head
+  __shared__ int64_t src[TS_MAX_D], dst[TS_MAX_D];  // pages' first bytes
+  __shared__ int src_off[TS_MAX_D], dst_off[TS_MAX_D], count;
   const int q = blockIdx.x, layer = blockIdx.y, t = threadIdx.x;
-  const int shift = p.c.page_shift, limit = p.max_blocks << shift;
-  const int n = p.n[q], count = min(p.path_len[q], TS_MAX_D);
-  const int len = max(p.len[q], 0);
-  const bool on = n >= 0 && count >= 0;
-  if (t < TS_MAX_D) {
-    int from = -1, to = -1;
-    if (on && t < count && len < limit) {
+  const int shift = p.c.page_shift, limit = p.max_blocks << shift, mask = (1 << shift) - 1;
+  if (t < 64) {
+    const int n = p.n[q], paths = p.path_len[q], given = p.len[q], len = max(given, 0);
+    const int node = t < TS_MAX_D ? p.path_nodes[q * TS_MAX_D + t] : 0;
+    const int one_up = __shfl_up(node, 1), before = t ? one_up : 0;
+    const bool on = n >= 0 && paths >= 0;
+    bool valid = on && t < min(paths, TS_MAX_D) && len < limit && node > before && node <= n && node < limit - len;
+    if (valid) {
       const int32_t* row = p.table + (size_t)q * p.max_blocks;
-      const int node = p.path_nodes[q * TS_MAX_D + t], before = t ? p.path_nodes[q * TS_MAX_D + t - 1] : 0;
-      if (node > before && node <= n && node < limit - len) {
-        const int a = len + node, b = len + 1 + t;  // b <= a: the path's nodes increase from 1 on
-        const int pa = kv_page(row, a >> shift, p.max_blocks, p.c.num_pages);
-        const int pb = b < limit ? kv_page(row, b >> shift, p.max_blocks, p.c.num_pages) : -1;
-        const int mask = (1 << shift) - 1;
-        if (pa >= 0 && pb >= 0) from = (pa << shift) + (a & mask), to = (pb << shift) + (b & mask);
+      const int a = len + node, b = len + 1 + t;  // b <= a: the path's nodes increase from 1 on
+      const int pa = kv_page(row, a >> shift, p.max_blocks, p.c.num_pages);
+      const int pb = b < limit ? kv_page(row, b >> shift, p.max_blocks, p.c.num_pages) : -1;
+      valid = pa >= 0 && pb >= 0;
+      if (valid) {
+        src[t] = (int64_t)pa * p.c.page_stride, src_off[t] = a & mask;
+        dst[t] = (int64_t)pb * p.c.page_stride, dst_off[t] = b & mask;
       }
     }
-    src[t] = from;
-    dst[t] = to;
+    const int kept = __builtin_ctzll(~__ballot(valid));  // up to the first that is not
+    if (t == 0) {
+      count = kept;
+      if (layer == 0) p.new_len[q] = on ? len + 1 + kept : given;
+    }
   }
   __syncthreads();
-  int kept = 0;
-  while (kept < TS_MAX_D && src[kept] >= 0) ++kept;
-  if (layer == 0 && t == 0) p.new_len[q] = on ? p.len[q] < 0 ? 1 + kept : p.len[q] + 1 + kept : p.len[q];
+  const int kept = count;
+  if (kept == 0) return;
   const int items = p.c.heads * kPieces;
-  const int64_t lay = (int64_t)layer * p.c.layer_stride;
-  for (int it = t; it < items; it += kRowThreads) {
+  char* pages = p.c.pages + (int64_t)layer * p.c.layer_stride;
+  for (int it = t; it < items; it += kAcceptThreads) {
     const int head = it / kPieces, piece = it % kPieces;
-    uint32_t w[TS_MAX_D];
-    auto place = [&](int slot) {
-      const int off = slot & ((1 << shift) - 1);
-      char* b = kv_block<D>(p.c, slot >> shift, head) + lay;
-      if (piece < kCodeWords) return b + KvBlock<D>::key_codes(off) + piece * 4;
-      if (piece < 2 * kCodeWords) return b + KvBlock<D>::value_codes(off, shift) + (piece - kCodeWords) * 4;
-      const int s = piece - 2 * kCodeWords;
-      if (s < kScaleHalves) return b + KvBlock<D>::key_scales(off, shift) + s * 2;
-      return b + KvBlock<D>::value_scales(off, shift) + (s - kScaleHalves) * 2;
-    };
-    const bool word = piece < 2 * kCodeWords;
-#pragma unroll
-    for (int j = 0; j < TS_MAX_D; ++j)
-      if (j < kept) {
-        const char* a = place(src[j]);
-        w[j] = word ? *reinterpret_cast<const uint32_t*>(a) : *reinterpret_cast<const uint16_t*>(a);
-      }
-#pragma unroll
-    for (int j = 0; j < TS_MAX_D; ++j)
-      if (j < kept) {
-        char* a = place(dst[j]);
-        if (word)
-          *reinterpret_cast<uint32_t*>(a) = w[j];
-        else
-          *reinterpret_cast<uint16_t*>(a) = (uint16_t)w[j];
-      }
+    char* base = pages + (int64_t)head * KvBlock<D>::bytes(shift);
+    if (piece < kCodes)
+      kv_move<16, D>(base, src, dst, src_off, dst_off, kept, KvBlock<D>::key_codes(0) + piece * 16, D / 2);
+    else if (piece < 2 * kCodes)
+      kv_move<16, D>(base, src, dst, src_off, dst_off, kept, KvBlock<D>::value_codes(0, shift) + (piece - kCodes) * 16, D / 2);
+    else
+      kv_move<D / 32, D>(base, src, dst, src_off, dst_off, kept,
+                         piece == 2 * kCodes ? KvBlock<D>::key_scales(0, shift) : KvBlock<D>::value_scales(0, shift), D / 32);
   }
 }
 

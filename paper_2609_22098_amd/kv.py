@@ -19,8 +19,10 @@ from __future__ import annotations
 
 import ctypes
 
+import torch
+
 from . import binding
-from .binding import TS_BF16, TS_F32, TS_MAX_D, TreeSparkError, _check, _torch  # noqa: F401
+from .binding import TS_BF16, TS_F32, TS_MAX_D, TreeSparkError, _check  # noqa: F401
 
 EXPORTED = ("ts_kv_block_bytes", "ts_kv_plan", "ts_kv_append", "ts_kv_read", "ts_kv_attention_workspace_size",
             "ts_kv_attention", "ts_kv_accept")
@@ -62,37 +64,40 @@ def lib():
     return _lib
 
 
+_I32 = torch.int32
+
+
 def _int32(name, t, shape, device):
     """The address of a contiguous int32 tensor of that shape on that GPU."""
-    if t.dtype is not _torch().int32 or tuple(t.shape) != shape or t.get_device() != device or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous int32 tensor {list(shape)} on cuda:{device} is needed, "
-                         f"got {t.dtype} {list(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is _I32 and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: a contiguous int32 tensor {list(shape)} on cuda:{device} is needed, got {t.dtype} "
+                     f"{list(t.shape)} on {t.device}")
 
 
-class _On:
-    """The device's current or the given stream, with the device current during the call."""
+def _public_stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
 
-    __slots__ = ("device", "stream", "before")
 
-    def __init__(self, device, stream):
-        cuda = _torch().cuda
-        if stream is None:
-            stream = cuda.current_stream(device)
-        elif stream.device_index != device:
-            raise ValueError(f"the stream is of cuda:{stream.device_index}, the tensors are on cuda:{device}")
-        self.device, self.stream = device, stream.cuda_stream
+# the handle of a device's current stream; the short way takes 0.1 us of the 1.2 us of the public one
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _public_stream)
 
-    def __enter__(self):
-        cuda = _torch().cuda
-        self.before = cuda.current_device()
-        if self.before != self.device:
-            cuda.set_device(self.device)
-        return self.stream
 
-    def __exit__(self, *_):
-        if self.before != self.device:
-            _torch().cuda.set_device(self.before)
+def _call(function, device, stream, *args):
+    """Calls a C entry on the device's current or the given stream, with the device current."""
+    if stream is None:
+        handle = _current_stream(device)
+    elif stream.device_index != device:
+        raise ValueError(f"the stream is of cuda:{stream.device_index}, the tensors are on cuda:{device}")
+    else:
+        handle = stream.cuda_stream
+    if torch.cuda.current_device() == device:
+        rc = function(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            rc = function(*args, handle)
+    if rc:
+        _check(rc)
 
 
 class Cache:
@@ -101,7 +106,6 @@ class Cache:
     of 16)."""
 
     def __init__(self, pages, page_size, heads, head_dim):
-        torch = _torch()
         if pages.dim() != 3 or pages.dtype is not torch.uint8 or not pages.is_cuda or pages.stride(2) != 1:
             raise ValueError("pages: a uint8 tensor [layers][num_pages][bytes] on a GPU is needed")
         block = block_bytes(page_size, head_dim)
@@ -111,6 +115,8 @@ class Cache:
         self.struct = CacheStruct(pages.data_ptr(), pages.stride(0), pages.stride(1), pages.shape[0], pages.shape[1],
                                   page_size, heads, head_dim)
         self._ref = ctypes.byref(self.struct)
+        self._row = (heads, head_dim)
+        self._sizes = {}  # workspace bytes by sizes
 
     @property
     def layers(self):
@@ -146,7 +152,6 @@ def block_bytes(page_size, head_dim):
 
 def empty_cache(layers, num_pages, page_size, heads, head_dim, device="cuda"):
     """A Cache in new memory."""
-    torch = _torch()
     pages = torch.zeros((layers, num_pages, heads * block_bytes(page_size, head_dim)), dtype=torch.uint8, device=device)
     return Cache(pages, page_size, heads, head_dim)
 
@@ -157,7 +162,6 @@ class Pool:
 
     def __init__(self, num_pages, R, max_blocks, page_size, device="cuda", free_pages=None, free_count=None, held=None,
                  table=None):
-        torch = _torch()
         given = (free_pages, free_count, held, table)
         if all(t is None for t in given):
             free_pages = torch.arange(num_pages, dtype=torch.int32, device=device)
@@ -176,82 +180,79 @@ class Pool:
 def plan(pool: Pool, length, n, cap, slots=True, out=None, stream=None):
     """ts_kv_plan: pages for the rows 0..n[q] behind length[q] tokens of every request.  Returns (slot [R][cap],
     granted [R]), int32; slot is None with slots=False (only the pages).  out = (slot, granted) reuses tensors."""
-    torch = _torch()
     R, d = pool.R, pool.device
     a_len, a_n = _int32("length", length, (R,), d), _int32("n", n, (R,), d)
     if out is None:
-        slot = torch.empty((R, cap), dtype=torch.int32, device=length.device) if slots else None
-        granted = torch.empty((R,), dtype=torch.int32, device=length.device)
+        slot = n.new_empty((R, cap)) if slots else None
+        granted = n.new_empty((R,))
     else:
         slot, granted = out
         _int32("granted", granted, (R,), d)
         if slot is not None:
             _int32("slot", slot, (R, cap), d)
     free_pages, free_count, held, table = pool._addr
-    with _On(d, stream) as s:
-        _check(lib().ts_kv_plan(a_len, a_n, R, cap, pool.page_size, pool.num_pages, pool.max_blocks, free_pages, free_count,
-                                held, table, slot.data_ptr() if slot is not None else None, granted.data_ptr(), s))
+    _call(lib().ts_kv_plan, d, stream, a_len, a_n, R, cap, pool.page_size, pool.num_pages, pool.max_blocks, free_pages,
+          free_count, held, table, slot.data_ptr() if slot is not None else None, granted.data_ptr())
     return slot, granted
 
 
 def _rows(name, t, cache):
-    """Address and row stride of keys or values [rows][heads][head_dim] (or [R][cap][heads][head_dim])."""
-    s = cache.struct
-    if t.shape[-2:] != (s.heads, s.head_dim) or t.dim() not in (3, 4) or t.get_device() != cache.device:
-        raise ValueError(f"{name}: [rows][{s.heads}][{s.head_dim}] on cuda:{cache.device} is needed, got {list(t.shape)} "
-                         f"on {t.device}")
-    st = t.stride()
-    if st[-1] != 1 or st[-2] != s.head_dim or (t.dim() == 4 and st[0] != st[1] * t.shape[1]):
+    """Row stride of keys or values [rows][heads][head_dim] (or [R][cap][heads][head_dim])."""
+    sh, st = t.shape, t.stride()
+    heads, D = cache._row
+    if len(sh) not in (3, 4) or sh[-1] != D or sh[-2] != heads or t.get_device() != cache.device:
+        raise ValueError(f"{name}: [rows][{heads}][{D}] on cuda:{cache.device} is needed, got {list(sh)} on {t.device}")
+    if st[-1] != 1 or (st[-2] != D and heads > 1) or (len(sh) == 4 and st[0] != st[1] * sh[1] and sh[0] > 1):
         raise ValueError(f"{name}: the heads of a row must be contiguous and rows evenly spaced, got strides {st}")
-    return t.data_ptr(), st[-3]
+    rows = sh[0] if len(sh) == 3 else sh[0] * sh[1]
+    return st[-3] if rows > 1 else max(st[-3], heads * D)
 
 
 def append(cache: Cache, k, v, slot, layer=0, stream=None):
     """ts_kv_append: rows' keys and values k, v [rows][heads][head_dim] (float32 or bfloat16; rows may be apart,
     as in a projection's output that holds both) into a layer of the cache, at slot (int32, one per row)."""
-    a_k, s_k = _rows("k", k, cache)
-    a_v, s_v = _rows("v", v, cache)
-    if k.dtype is not v.dtype or k.shape[:-2] != v.shape[:-2]:
-        raise ValueError("k and v must have one dtype and as many rows")
+    s_k, s_v = _rows("k", k, cache), _rows("v", v, cache)
     rows = slot.numel()
-    if k.shape[:-2].numel() != rows:
-        raise ValueError(f"{rows} slots for {k.shape[:-2].numel()} rows")
-    a_slot = _int32("slot", slot, tuple(slot.shape), cache.device)
-    with _On(cache.device, stream) as s:
-        _check(lib().ts_kv_append(cache.ref(), layer, a_k, a_v, binding._dtype_code(k), s_k, s_v, a_slot, rows, s))
+    if k.dtype is not v.dtype or k.shape != v.shape:
+        raise ValueError("k and v must have one dtype and as many rows")
+    if k.numel() != rows * cache._row[0] * cache._row[1]:
+        raise ValueError(f"{rows} slots for keys {list(k.shape)}")
+    _call(lib().ts_kv_append, cache.device, stream, cache._ref, layer, k.data_ptr(), v.data_ptr(), binding._dtype_code(k),
+          s_k, s_v, _int32("slot", slot, slot.shape, cache.device), rows)
 
 
 def read(cache: Cache, slot, layer=0, layers=None, dtype=None, out=None, stream=None):
     """ts_kv_read: the rows at slot as (k, v) [layers][rows][heads][head_dim], of `layers` layers from `layer` on
     (None: all that follow).  out = (k, v) reuses tensors, either of which may be None; without it rows that have no
     slot are zero.  dtype: float32 or bfloat16 (the default)."""
-    torch = _torch()
-    c = cache.struct
-    layers = c.layers - layer if layers is None else layers
-    rows = slot.numel()
-    shape = (layers, rows, c.heads, c.head_dim)
+    layers = cache.struct.layers - layer if layers is None else layers
+    rows, d = slot.numel(), cache.device
+    shape = (layers, rows) + cache._row
+    a_slot = _int32("slot", slot, slot.shape, d)
     if out is None:
         out = tuple(torch.zeros(shape, dtype=dtype or torch.bfloat16, device=slot.device) for _ in range(2))
     k, v = out
     one = k if k is not None else v
-    for t in out:
-        if t is not None and (tuple(t.shape) != shape or t.get_device() != cache.device or not t.is_contiguous()
-                              or t.dtype is not one.dtype):
-            raise ValueError(f"out: contiguous tensors {list(shape)} of one dtype on cuda:{cache.device} are needed")
     if one is None:
         return out
-    a_slot = _int32("slot", slot, tuple(slot.shape), cache.device)
-    with _On(cache.device, stream) as s:
-        _check(lib().ts_kv_read(cache.ref(), layer, layers, a_slot, rows, k.data_ptr() if k is not None else None,
-                                v.data_ptr() if v is not None else None, binding._dtype_code(one), s))
+    for t in out:
+        if t is not None and (t.shape != shape or t.get_device() != d or not t.is_contiguous() or t.dtype is not one.dtype):
+            raise ValueError(f"out: contiguous tensors {list(shape)} of one dtype on cuda:{d} are needed")
+    _call(lib().ts_kv_read, d, stream, cache._ref, layer, layers, a_slot, rows, k.data_ptr() if k is not None else None,
+          v.data_ptr() if v is not None else None, binding._dtype_code(one))
     return k, v
 
 
 def attention_workspace_size(cache: Cache, R, cap, q_heads, dtype):
     """ts_kv_attention_workspace_size for queries of a torch dtype."""
-    code = TS_BF16 if dtype is _torch().bfloat16 else TS_F32
-    with _On(cache.device, None):
-        return lib().ts_kv_attention_workspace_size(cache.ref(), R, cap, q_heads, code)
+    key = R, cap, q_heads, dtype
+    size = cache._sizes.get(key)
+    if size is None:
+        with torch.cuda.device(cache.device):
+            size = lib().ts_kv_attention_workspace_size(cache._ref, R, cap, q_heads,
+                                                        TS_BF16 if dtype is torch.bfloat16 else TS_F32)
+        cache._sizes[key] = size
+    return size
 
 
 def attention(cache: Cache, q, length, n, table, mask=None, scale=None, layer=0, out=None, lse=None, workspace=None,
@@ -260,40 +261,38 @@ def attention(cache: Cache, q, length, n, table, mask=None, scale=None, layer=0,
     [R][max_blocks], mask the [R][cap][W] words of binding.tree_mask or None for chains (causal).  scale: head_dim
     ** -0.5 by default.  Returns (out, lse): out like q, contiguous; lse float32 [R][cap][q_heads] if given, else None.
     Rows past n[q] of given tensors are left as they were; those of a new out are zero."""
-    torch = _torch()
-    c, d = cache.struct, cache.device
-    if q.dim() != 4 or q.shape[3] != c.head_dim or q.get_device() != d:
-        raise ValueError(f"q: [R][cap][q_heads][{c.head_dim}] on cuda:{d} is needed, got {list(q.shape)} on {q.device}")
-    R, cap, q_heads, D = q.shape
-    st = q.stride()
+    d, sh, st = cache.device, q.shape, q.stride()
+    if len(sh) != 4 or sh[3] != cache._row[1] or q.get_device() != d:
+        raise ValueError(f"q: [R][cap][q_heads][{cache._row[1]}] on cuda:{d} is needed, got {list(sh)} on {q.device}")
+    R, cap, q_heads, D = sh
     if st[3] != 1 or (st[2] != D and q_heads > 1) or (st[0] != st[1] * cap and R > 1):
         raise ValueError(f"q: the heads of a row must be contiguous and rows evenly spaced, got strides {st}")
     dtype = binding._dtype_code(q)
     if table.dim() != 2:
         raise ValueError("table: [R][max_blocks] is needed")
     max_blocks = table.shape[1]
-    a_table = _int32("table", table, (R, max_blocks), d)
-    a_len, a_n = _int32("length", length, (R,), d), _int32("n", n, (R,), d)
-    a_mask = _int32("mask", mask, (R, cap, (cap + 31) // 32), d) if mask is not None else None
     if out is None:
-        out = torch.zeros((R, cap, q_heads, D), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != d or not out.is_contiguous():
-        raise ValueError(f"out: a contiguous {q.dtype} tensor {list(q.shape)} on cuda:{d} is needed")
-    if lse is not None and (lse.dtype is not torch.float32 or tuple(lse.shape) != (R, cap, q_heads)
-                            or lse.get_device() != d or not lse.is_contiguous()):
-        raise ValueError(f"lse: a contiguous float32 tensor {[R, cap, q_heads]} on cuda:{d} is needed")
-    with _On(d, stream) as s:
-        if workspace is None:
-            size = lib().ts_kv_attention_workspace_size(cache.ref(), R, cap, q_heads, dtype)
-            with torch.cuda.stream(stream or torch.cuda.current_stream(d)):  # freed memory is reused in its order
-                workspace = torch.empty((max(size, 1),), dtype=torch.uint8, device=q.device)
-        elif workspace.get_device() != d or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
-            raise ValueError(f"workspace: a contiguous uint8 tensor on cuda:{d} is needed")
-        _check(lib().ts_kv_attention(cache.ref(), layer, q.data_ptr(), dtype, st[1] if cap > 1 or R > 1 else q_heads * D, q_heads,
-                                     a_len, a_n, R, cap, a_table, max_blocks, a_mask,
-                                     D ** -0.5 if scale is None else scale, out.data_ptr(),
-                                     lse.data_ptr() if lse is not None else None, workspace.data_ptr(),
-                                     workspace.numel(), s))
+        out = torch.zeros(sh, dtype=q.dtype, device=q.device)
+    elif out.shape != sh or out.dtype is not q.dtype or out.get_device() != d or not out.is_contiguous():
+        raise ValueError(f"out: a contiguous {q.dtype} tensor {list(sh)} on cuda:{d} is needed")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != sh[:3] or lse.get_device() != d
+                            or not lse.is_contiguous()):
+        raise ValueError(f"lse: a contiguous float32 tensor {list(sh[:3])} on cuda:{d} is needed")
+    if workspace is None:
+        size = max(attention_workspace_size(cache, R, cap, q_heads, q.dtype), 1)
+        if stream is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+        else:
+            with torch.cuda.stream(stream):  # freed memory is then reused in that stream's order
+                workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != d or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise ValueError(f"workspace: a contiguous uint8 tensor on cuda:{d} is needed")
+    _call(lib().ts_kv_attention, d, stream, cache._ref, layer, q.data_ptr(), dtype,
+          st[1] if cap > 1 else st[0] if R > 1 else q_heads * D, q_heads, _int32("length", length, (R,), d),
+          _int32("n", n, (R,), d), R, cap, _int32("table", table, (R, max_blocks), d), max_blocks,
+          None if mask is None else _int32("mask", mask, (R, cap, (cap + 31) // 32), d),
+          D ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr() if lse is not None else None,
+          workspace.data_ptr(), workspace.numel())
     return out, lse
 
 
@@ -301,7 +300,6 @@ def accept(cache: Cache, length, n, table, path_nodes, path_len, new_length=None
     """ts_kv_accept: the accepted paths' rows, in every layer, moved behind the contexts.  path_nodes [R][16] and
     path_len [R] as binding.verify returns them (numpy arrays are copied to the GPU) or int32 GPU tensors.  Returns
     the new lengths [R]."""
-    torch = _torch()
     d = cache.device
     if table.dim() != 2:
         raise ValueError("table: [R][max_blocks] is needed")
@@ -311,10 +309,8 @@ def accept(cache: Cache, length, n, table, path_nodes, path_len, new_length=None
     if not isinstance(path_len, torch.Tensor):
         path_len = torch.from_numpy(path_len).to(table.device)
     if new_length is None:
-        new_length = torch.empty((R,), dtype=torch.int32, device=table.device)
-    with _On(d, stream) as s:
-        _check(lib().ts_kv_accept(cache.ref(), _int32("length", length, (R,), d), _int32("n", n, (R,), d), R,
-                                  _int32("table", table, (R, max_blocks), d), max_blocks,
-                                  _int32("path_nodes", path_nodes, (R, TS_MAX_D), d), _int32("path_len", path_len, (R,), d),
-                                  _int32("new_length", new_length, (R,), d), s))
+        new_length = length.new_empty((R,))
+    _call(lib().ts_kv_accept, d, stream, cache._ref, _int32("length", length, (R,), d), _int32("n", n, (R,), d), R,
+          _int32("table", table, (R, max_blocks), d), max_blocks, _int32("path_nodes", path_nodes, (R, TS_MAX_D), d),
+          _int32("path_len", path_len, (R,), d), _int32("new_length", new_length, (R,), d))
     return new_length
