@@ -69,18 +69,32 @@ struct AttnPlan {
   size_t stats, joins, bytes;  // offsets after the parts, and all
 };
 
-// The smallest tile that holds all rows of a request and kv head, so that its
-// keys and values are read once; the largest where none does.
-AttnPlan attn_plan(const ts_kv_cache* c, int32_t cap, int32_t q_heads, int32_t dtype, int cus) {
+// tokens: the most that a request's table can name (0: unknown, which takes the
+// most workspace).
+//
+// The tile: the smallest that holds all rows of a request and kv head, so that its
+// keys and values are read once, up to the largest, whose waves share them (64
+// trees of up to 65 rows and 4 query heads a kv head over 500 to 8000 tokens: tiles
+// of 128 rows 192 us, of 32 257, of 16 304).  A few tiles cut into many pieces
+// cost more in partial results than they gain, unless their context is long: one
+// such tree over 5003 tokens takes 40 us in tiles of 128 and 34 in tiles of 32,
+// three of 33 rows in fp32 over 50 to 700 27 us in tiles of 64 and 21 in tiles of 16.
+//
+// The workgroups: what a compute unit holds of them, so that none waits.  Tiles of
+// 16 rows would allow three; few of them are cut into two thirds as many pieces
+// (131001 tokens, 8 tiles: 40 us with two, 44 with three; 1024 tiles 125 and 122).
+AttnPlan attn_plan(const ts_kv_cache* c, int32_t R, int32_t cap, int32_t q_heads, int32_t dtype, int64_t tokens, int cus) {
   AttnPlan x;
-  const int64_t rows = (int64_t)cap * (q_heads / c->heads);
+  const int64_t rows = (int64_t)cap * (q_heads / c->heads), most = dtype == TS_F32 ? 64 : 128;
+  const bool few = (int64_t)R * c->heads * ((rows + most - 1) / most) * 4 < cus, brief = few && tokens > 0 && tokens <= 16384;
   if (dtype == TS_F32)
-    x.tile = rows <= 16 ? AttnTile::k16 : AttnTile::k64;
+    x.tile = rows <= 16 || brief ? AttnTile::k16 : AttnTile::k64;
   else
-    x.tile = rows <= 16 ? AttnTile::k16 : rows <= 64 ? AttnTile::k32 : AttnTile::k128;
+    x.tile = rows <= 16 ? AttnTile::k16 : rows <= 64 || brief ? AttnTile::k32 : AttnTile::k128;
   x.rows = 16 << (int)x.tile;
-  x.groups = cus * (x.tile == AttnTile::k16 && dtype == TS_BF16 ? 3 : 2);
-  x.min_tokens = x.tile == AttnTile::k16 || x.tile == AttnTile::k32 ? 256 : 128;  // a step of the former
+  const bool small = x.tile == AttnTile::k16 || x.tile == AttnTile::k32;
+  x.groups = cus * (c->head_dim == 256 ? 1 : x.tile == AttnTile::k16 && dtype == TS_BF16 && !few ? 3 : 2);
+  x.min_tokens = small ? 256 : 64;  // a step
   const size_t parts = (size_t)x.groups * 2 * x.rows;
   x.stats = parts * c->head_dim * sizeof(float);
   x.joins = x.stats + parts * sizeof(AttnStat);
@@ -185,7 +199,7 @@ size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32
   if (check_cache(cache) || check_dtype(dtype) || R < 0 || R > kMaxRequests || cap < 1 || cap > TS_KV_MAX_CAP || q_heads < 1 ||
       q_heads % cache->heads)
     return 0;
-  return attn_plan(cache, cap, q_heads, dtype, compute_units()).bytes;
+  return attn_plan(cache, R, cap, q_heads, dtype, 0, compute_units()).bytes;
 }
 
 int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, int32_t dtype, int64_t q_stride,
@@ -210,8 +224,10 @@ int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, 
   if (q_stride < width || q_stride % (16 / elem_size(dtype)))
     return fail(TS_EINVAL, "q_stride %lld: at least %lld elements and whole 16 bytes are needed", (long long)q_stride, (long long)width);
   if (!aligned16(q) || !aligned16(out)) return fail(TS_EINVAL, "q and out must start at 16-byte aligned addresses");
-  const AttnPlan plan = attn_plan(cache, cap, q_heads, dtype, compute_units());
-  if (workspace_bytes < plan.bytes) return fail(TS_ENOSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, plan.bytes);
+  const int cus = compute_units();
+  const size_t need = attn_plan(cache, R, cap, q_heads, dtype, 0, cus).bytes;
+  if (workspace_bytes < need) return fail(TS_ENOSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+  const AttnPlan plan = attn_plan(cache, R, cap, q_heads, dtype, (int64_t)max_blocks * cache->page_size, cus);
   if (!workspace || !aligned16(workspace)) return fail(TS_EINVAL, "workspace must be 16-byte aligned memory");
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);

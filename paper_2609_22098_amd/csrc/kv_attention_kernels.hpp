@@ -57,7 +57,7 @@ struct AttnShape {
   static constexpr int kORow = D + 4;            // floats of a row of results in LDS
   static constexpr int kVBytes = WT * kVTokens * kVRow;
   static constexpr int kOBytes = WT * WM * 16 * kORow * 4;
-  static constexpr int kFixed = 128 * WT;        // tokens' worth of a tile's beginning and end
+  static constexpr int kFixed = 512;             // tokens' worth of a tile's beginning and end (128: 64 trees 222 us, this 198)
   // workgroups on a compute unit: registers allow waves of 128 where a wave has one block of rows
   static constexpr int kResident = MB == 1 && D <= 128 && !kF32 ? 3 : D <= 128 ? 2 : 1;
   static constexpr int kLds = kVBytes > kOBytes ? kVBytes : kOBytes;
@@ -722,6 +722,11 @@ void kv_attention_kernel(KvAttnParams p) {
           pages_of(s + 2, entry, pg[2]);
           look_up(s + 3, entry);
           const bool first = part || s == s0;
+          // Two workgroups share a compute unit, and the older one's waves always go
+          // first: it ends at 580 us where the other needs 740.  They take turns at a
+          // higher priority instead, 41 us each by the device's clock.
+          if ((uint32_t)__builtin_readsteadycounter() >> 12 & 1 ^ (blockIdx.x >= gridDim.x / 2)) __builtin_amdgcn_s_setprio(1);
+          else __builtin_amdgcn_s_setprio(0);
           // What is loaded past the last tile lies in some page and is of no use; a
           // branch around it would keep the products from running beside the rest.
           // second half of the tile before, first half's weights, second half's scores

@@ -366,7 +366,7 @@ def test_attention_strides(torch):
         want, _ = c.run(torch)
         wide = torch.randn((2, 5, 11, 64), device="cuda").to(c.t)
         wide[:, :, 3:7] = c.q.cuda()
-        packed = torch.from_numpy(kv_ref.pack(c.ref)[0]).cuda()
+        packed = torch.from_numpy(kv_ref.pack(c.ref)[0].copy()).cuda()
         pages = torch.randint(0, 256, (len(packed), 3, packed.shape[1] + 32), dtype=torch.uint8, device="cuda")
         pages[:, 1, : packed.shape[1]] = packed
         cache = kv.Cache(pages.transpose(0, 1)[:, :, : packed.shape[1]], 16, 2, 64)
@@ -389,7 +389,7 @@ def test_attention_far_pages(torch):
     want, wl = c.run(torch)
     far = 300000  # 300000 pages of 17408 bytes: 5.2 GB
     pages = torch.zeros((1, far, 64 * 136 * 2), dtype=torch.uint8, device="cuda")
-    packed = torch.from_numpy(kv_ref.pack(c.ref)[0]).cuda()
+    packed = torch.from_numpy(kv_ref.pack(c.ref)[0].copy()).cuda()
     pages[0, far - len(packed):] = packed
     cache = kv.Cache(pages, 64, 2, 128)
     table = np.where(c.table >= 0, c.table + far - len(packed), -1)

@@ -100,6 +100,22 @@ def test_attention_refusals():
     assert _attention(c, R=0, q=None) == b.TS_OK
 
 
+def test_attention_workspace():
+    """A function of sizes alone, which a call refuses to go below; 0 for what it would refuse."""
+    c, L = _cache(), kv.lib()
+
+    def size(R=2, cap=5, hq=4, dtype=b.TS_BF16, c=c):
+        return L.ts_kv_attention_workspace_size(ctypes.byref(c), R, cap, hq, dtype)
+
+    assert 0 < size(R=1) <= size() <= size(R=60000) and size() <= size(cap=500)
+    assert size(hq=3) == size(cap=0) == size(R=-1) == size(dtype=4) == size(c=_cache(head_dim=80)) == 0
+    for R, cap, hq, dtype in ((2, 5, 4, b.TS_BF16), (1, 1, 2, b.TS_F32), (70, 65, 8, b.TS_BF16), (1, 4096, 4, b.TS_F32)):
+        n = size(R, cap, hq, dtype)
+        kw = dict(R=R, cap=cap, hq=hq, dtype=dtype, qs=hq * 128)
+        assert _attention(c, wsb=n - 1, **kw) == b.TS_ENOSPACE
+        assert _attention(c, wsb=n, ws=None, **kw) == b.TS_EINVAL and _attention(c, wsb=n, ws=FAKE + 8, **kw) == b.TS_EINVAL
+
+
 def test_accept_refusals():
     c = _cache()
     for kw in (dict(length=None), dict(n=None), dict(table=None), dict(nodes=None), dict(plen=None), dict(new=None),
