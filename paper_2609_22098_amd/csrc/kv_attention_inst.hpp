@@ -10,6 +10,7 @@ namespace ts {
 template <typename S>
 static void launch_attention_shape(const KvAttnParams& p, int groups, hipStream_t s) {
   hipLaunchKernelGGL((kv_attention_kernel<S>), dim3(groups), dim3(S::kThreads), 0, s, p);
+  if (p.whole_tiles) return;
   constexpr int kThreads = S::kRows > 32 ? 256 : 512, kUnit = S::kRows > 32 ? 1024 / S::D : 4, kMost = S::kRows > 32 ? 2048 : 1024;
   const int units = groups * (S::kRows / kUnit);
   hipLaunchKernelGGL((kv_join_kernel<typename S::TE, S::D, kThreads, kUnit>), dim3(units < kMost ? units : kMost), dim3(kThreads), 0, s, p,

@@ -26,6 +26,7 @@
 // Work.  The steps of all tiles of all requests, in one line, are cut into
 // equal pieces, one a workgroup: no length decides the balance.  A tile
 // that a cut goes through leaves partial results, and a second kernel joins them.
+// Where a table names few tokens, nothing is cut: a workgroup takes a tile.
 #pragma once
 
 #include "kv_format.hpp"
@@ -286,30 +287,42 @@ void kv_attention_kernel(KvAttnParams p) {
     }
     return incl;
   };
-  int64_t v, all, incl = scan(0, v, all), total = all;
-  for (int q0 = S::kThreads; q0 < p.R; q0 += S::kThreads) {
-    scan(q0, v, all);
-    total += all;
-  }
-  const int64_t per = max((total + groups - 1) / groups, (int64_t)p.min_tokens * p.group);
-  const int64_t begin = per * w, end = min(begin + per, total);
-  if (tid == 0) p.joins[w].q = -1;
-  if (begin >= end) return;
-  int64_t before = 0;
-  for (int q0 = 0; q0 < p.R; q0 += S::kThreads) {
-    if (p.R > S::kThreads) incl = scan(q0, v, all);
-    if (before + incl - v <= begin && begin < before + incl) {
-      found = q0 + tid;
-      found_at = before + incl - v;
+  int q;
+  int64_t at, begin, end, per;  // of request q's first step; the piece and every piece's length
+  if (p.whole_tiles) {
+    // short contexts: a tile a workgroup (of whole_tiles for each request and kv head)
+    q = w / (p.c.heads * p.whole_tiles);
+    const int head = w / p.whole_tiles % p.c.heads, rt = w % p.whole_tiles;
+    const AttnReq<S> r(p, q);
+    if (rt >= r.tiles) return;
+    at = -(head * r.all + r.before(rt));
+    begin = 0, end = per = r.first + r.more * rt;
+  } else {
+    int64_t v, all, incl = scan(0, v, all), total = all;
+    for (int q0 = S::kThreads; q0 < p.R; q0 += S::kThreads) {
+      scan(q0, v, all);
+      total += all;
     }
-    before += all;
+    per = max((total + groups - 1) / groups, (int64_t)p.min_tokens * p.group);
+    begin = per * w, end = min(begin + per, total);
+    if (tid == 0) p.joins[w].q = -1;
+    if (begin >= end) return;
+    int64_t before = 0;
+    for (int q0 = 0; q0 < p.R; q0 += S::kThreads) {
+      if (p.R > S::kThreads) incl = scan(q0, v, all);
+      if (before + incl - v <= begin && begin < before + incl) {
+        found = q0 + tid;
+        found_at = before + incl - v;
+      }
+      before += all;
+    }
+    __syncthreads();
+    q = __builtin_amdgcn_readfirstlane(found);
+    at = found_at;
   }
-  __syncthreads();
-  int q = __builtin_amdgcn_readfirstlane(found);
-  int64_t at = found_at;  // of request q's first step
 
   const int g_rows = p.group;
-  for (int64_t pos = begin; pos < end;) {
+  for (int64_t pos = begin; pos < end && q < p.R;) {
     const AttnReq<S> r(p, q);
     if (pos >= at + r.all * p.c.heads) {
       at += r.all * p.c.heads;
