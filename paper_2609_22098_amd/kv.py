@@ -14,6 +14,8 @@ uint8 on one GPU, and a call that does not fit raises before anything is launche
         kv.append(cache, k, v, slot, layer=layer)           # k, v [R * cap][heads][head_dim]
         out, _ = kv.attention(cache, q, length, granted, pool.table, mask=mask, layer=layer)
     length = kv.accept(cache, length, granted, pool.table, path_nodes, path_len)
+
+A call runs on the tensors' device, on its current stream or the given one.
 """
 from __future__ import annotations
 
@@ -83,14 +85,9 @@ def _public_stream(device):
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _public_stream)
 
 
-def _call(function, device, stream, *args):
-    """Calls a C entry on the device's current or the given stream, with the device current."""
-    if stream is None:
-        handle = _current_stream(device)
-    elif stream.device_index != device:
-        raise ValueError(f"the stream is of cuda:{stream.device_index}, the tensors are on cuda:{device}")
-    else:
-        handle = stream.cuda_stream
+def _call(function, device, *args):
+    """Calls a C entry on the device's current stream, with the device current."""
+    handle = _current_stream(device)
     if torch.cuda.current_device() == device:
         rc = function(*args, handle)
     else:
@@ -98,6 +95,13 @@ def _call(function, device, stream, *args):
             rc = function(*args, handle)
     if rc:
         _check(rc)
+
+
+def _on(stream, device):
+    """The given stream as the current one: what a call allocates or fills is then in that stream's order too."""
+    if stream.device_index != device:
+        raise ValueError(f"the stream is of cuda:{stream.device_index}, the tensors are on cuda:{device}")
+    return torch.cuda.stream(stream)
 
 
 class Cache:
@@ -180,6 +184,9 @@ class Pool:
 def plan(pool: Pool, length, n, cap, slots=True, out=None, stream=None):
     """ts_kv_plan: pages for the rows 0..n[q] behind length[q] tokens of every request.  Returns (slot [R][cap],
     granted [R]), int32; slot is None with slots=False (only the pages).  out = (slot, granted) reuses tensors."""
+    if stream is not None:
+        with _on(stream, pool.device):
+            return plan(pool, length, n, cap, slots, out)
     R, d = pool.R, pool.device
     a_len, a_n = _int32("length", length, (R,), d), _int32("n", n, (R,), d)
     if out is None:
@@ -191,7 +198,7 @@ def plan(pool: Pool, length, n, cap, slots=True, out=None, stream=None):
         if slot is not None:
             _int32("slot", slot, (R, cap), d)
     free_pages, free_count, held, table = pool._addr
-    _call(lib().ts_kv_plan, d, stream, a_len, a_n, R, cap, pool.page_size, pool.num_pages, pool.max_blocks, free_pages,
+    _call(lib().ts_kv_plan, d, a_len, a_n, R, cap, pool.page_size, pool.num_pages, pool.max_blocks, free_pages,
           free_count, held, table, slot.data_ptr() if slot is not None else None, granted.data_ptr())
     return slot, granted
 
@@ -211,13 +218,16 @@ def _rows(name, t, cache):
 def append(cache: Cache, k, v, slot, layer=0, stream=None):
     """ts_kv_append: rows' keys and values k, v [rows][heads][head_dim] (float32 or bfloat16; rows may be apart,
     as in a projection's output that holds both) into a layer of the cache, at slot (int32, one per row)."""
+    if stream is not None:
+        with _on(stream, cache.device):
+            return append(cache, k, v, slot, layer)
     s_k, s_v = _rows("k", k, cache), _rows("v", v, cache)
     rows = slot.numel()
     if k.dtype is not v.dtype or k.shape != v.shape:
         raise ValueError("k and v must have one dtype and as many rows")
     if k.numel() != rows * cache._row[0] * cache._row[1]:
         raise ValueError(f"{rows} slots for keys {list(k.shape)}")
-    _call(lib().ts_kv_append, cache.device, stream, cache._ref, layer, k.data_ptr(), v.data_ptr(), binding._dtype_code(k),
+    _call(lib().ts_kv_append, cache.device, cache._ref, layer, k.data_ptr(), v.data_ptr(), binding._dtype_code(k),
           s_k, s_v, _int32("slot", slot, slot.shape, cache.device), rows)
 
 
@@ -225,6 +235,9 @@ def read(cache: Cache, slot, layer=0, layers=None, dtype=None, out=None, stream=
     """ts_kv_read: the rows at slot as (k, v) [layers][rows][heads][head_dim], of `layers` layers from `layer` on
     (None: all that follow).  out = (k, v) reuses tensors, either of which may be None; without it rows that have no
     slot are zero.  dtype: float32 or bfloat16 (the default)."""
+    if stream is not None:
+        with _on(stream, cache.device):
+            return read(cache, slot, layer, layers, dtype, out)
     layers = cache.struct.layers - layer if layers is None else layers
     rows, d = slot.numel(), cache.device
     shape = (layers, rows) + cache._row
@@ -238,7 +251,7 @@ def read(cache: Cache, slot, layer=0, layers=None, dtype=None, out=None, stream=
     for t in out:
         if t is not None and (t.shape != shape or t.get_device() != d or not t.is_contiguous() or t.dtype is not one.dtype):
             raise ValueError(f"out: contiguous tensors {list(shape)} of one dtype on cuda:{d} are needed")
-    _call(lib().ts_kv_read, d, stream, cache._ref, layer, layers, a_slot, rows, k.data_ptr() if k is not None else None,
+    _call(lib().ts_kv_read, d, cache._ref, layer, layers, a_slot, rows, k.data_ptr() if k is not None else None,
           v.data_ptr() if v is not None else None, binding._dtype_code(one))
     return k, v
 
@@ -261,6 +274,9 @@ def attention(cache: Cache, q, length, n, table, mask=None, scale=None, layer=0,
     [R][max_blocks], mask the [R][cap][W] words of binding.tree_mask or None for chains (causal).  scale: head_dim
     ** -0.5 by default.  Returns (out, lse): out like q, contiguous; lse float32 [R][cap][q_heads] if given, else None.
     Rows past n[q] of given tensors are left as they were; those of a new out are zero."""
+    if stream is not None:
+        with _on(stream, cache.device):
+            return attention(cache, q, length, n, table, mask, scale, layer, out, lse, workspace)
     d, sh, st = cache.device, q.shape, q.stride()
     if len(sh) != 4 or sh[3] != cache._row[1] or q.get_device() != d:
         raise ValueError(f"q: [R][cap][q_heads][{cache._row[1]}] on cuda:{d} is needed, got {list(sh)} on {q.device}")
@@ -279,15 +295,11 @@ def attention(cache: Cache, q, length, n, table, mask=None, scale=None, layer=0,
                             or not lse.is_contiguous()):
         raise ValueError(f"lse: a contiguous float32 tensor {list(sh[:3])} on cuda:{d} is needed")
     if workspace is None:
-        size = max(attention_workspace_size(cache, R, cap, q_heads, q.dtype), 1)
-        if stream is None:
-            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
-        else:
-            with torch.cuda.stream(stream):  # freed memory is then reused in that stream's order
-                workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(attention_workspace_size(cache, R, cap, q_heads, q.dtype), 1), dtype=torch.uint8,
+                                device=q.device)
     elif workspace.get_device() != d or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise ValueError(f"workspace: a contiguous uint8 tensor on cuda:{d} is needed")
-    _call(lib().ts_kv_attention, d, stream, cache._ref, layer, q.data_ptr(), dtype,
+    _call(lib().ts_kv_attention, d, cache._ref, layer, q.data_ptr(), dtype,
           st[1] if cap > 1 else st[0] if R > 1 else q_heads * D, q_heads, _int32("length", length, (R,), d),
           _int32("n", n, (R,), d), R, cap, _int32("table", table, (R, max_blocks), d), max_blocks,
           None if mask is None else _int32("mask", mask, (R, cap, (cap + 31) // 32), d),
@@ -300,6 +312,9 @@ def accept(cache: Cache, length, n, table, path_nodes, path_len, new_length=None
     """ts_kv_accept: the accepted paths' rows, in every layer, moved behind the contexts.  path_nodes [R][16] and
     path_len [R] as binding.verify returns them (numpy arrays are copied to the GPU) or int32 GPU tensors.  Returns
     the new lengths [R]."""
+    if stream is not None:
+        with _on(stream, cache.device):
+            return accept(cache, length, n, table, path_nodes, path_len, new_length)
     d = cache.device
     if table.dim() != 2:
         raise ValueError("table: [R][max_blocks] is needed")
@@ -310,7 +325,7 @@ def accept(cache: Cache, length, n, table, path_nodes, path_len, new_length=None
         path_len = torch.from_numpy(path_len).to(table.device)
     if new_length is None:
         new_length = length.new_empty((R,))
-    _call(lib().ts_kv_accept, d, stream, cache._ref, _int32("length", length, (R,), d), _int32("n", n, (R,), d), R,
+    _call(lib().ts_kv_accept, d, cache._ref, _int32("length", length, (R,), d), _int32("n", n, (R,), d), R,
           _int32("table", table, (R, max_blocks), d), max_blocks, _int32("path_nodes", path_nodes, (R, TS_MAX_D), d),
           _int32("path_len", path_len, (R,), d), _int32("new_length", new_length, (R,), d))
     return new_length

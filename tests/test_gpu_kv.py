@@ -158,7 +158,7 @@ def test_rows_keep_their_neighbours(torch):
 class Case:
     """A batch: cache, tables with scattered pages, queries, masks, and the oracle's answer."""
 
-    def __init__(self, torch, lens, ns, cap, hq, heads, D, page, dtype, mask, seed=0, layers=1, stretch=0, kscale=1.0):
+    def __init__(self, torch, lens, ns, cap, hq, heads, D, page, dtype, mask, seed=0, layers=1, reach=0, kscale=1.0):
         from paper_2609_22098_amd import kv
         rng = np.random.default_rng(seed)
         self.lens, self.ns, self.cap, self.D, self.dtype = np.array(lens), np.array(ns), cap, D, dtype
@@ -167,7 +167,7 @@ class Case:
         need = -(-(self.lens + self.rows) // page)
         pages = int(need.sum()) + 2
         ids = rng.permutation(pages)
-        self.blocks = int(need.max()) + stretch
+        self.blocks = max(int(need.max()), -(-reach // page))  # a table that names more tokens than there are
         self.table = np.full((R, self.blocks), -1, np.int64)
         at = 0
         for q in range(R):
@@ -285,16 +285,39 @@ SHAPES = [  # lens, n, cap, hq, heads, D, page
 @pytest.mark.parametrize("shape", range(len(SHAPES)))
 def test_attention(torch, shape, mask, dtype):
     """Chains and trees over contexts of no token to some thousand, groups of every kind, pages that end inside
-    a tile, requests that sit out, counts above the capacity."""
+    a tile, requests that sit out, counts above the capacity; tables that name few tokens, more, and many (the
+    work is then cut otherwise, into tiles of other sizes)."""
     lens, n, cap, hq, heads, D, page = SHAPES[shape]
-    Case(torch, lens, n, cap, hq, heads, D, page, dtype, mask, seed=shape, layers=1 + shape % 2, stretch=shape % 3).check(torch)
+    for reach in (0, 1200, 17000):
+        Case(torch, lens, n, cap, hq, heads, D, page, dtype, mask, seed=shape, layers=1 + shape % 2, reach=reach).check(torch)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,hi,cap,hq,heads,D,page", [(300, 90, 1, 2, 1, 64, 16), (300, 70, 5, 8, 2, 64, 64), (520, 40, 3, 44, 1, 128, 32),
+                                                      (1, 20000, 1, 4, 1, 128, 64), (2, 9000, 1, 1, 1, 256, 16), (1, 6000, 40, 8, 1, 128, 64),
+                                                      (3, 2500, 7, 4, 2, 256, 128)])
+def test_attention_cuts(torch, R, hi, cap, hq, heads, D, page, dtype):
+    """More requests than a workgroup has threads; a context that is cut into more pieces than a wave has lanes."""
+    rng = np.random.default_rng(R + hi)
+    lens, n = rng.integers(0, hi + 1, R), rng.integers(-1, cap, R)
+    lens[0], n[0] = hi, cap - 1
+    Case(torch, lens, n, cap, hq, heads, D, page, dtype, cap > 1, seed=R, reach=17000).check(torch)
+
+
+def test_attention_scale_of_zero(torch):
+    """Every visible token has the same weight; hidden ones still have none."""
+    for dtype in ("bf16", "f32"):
+        for reach in (0, 17000):
+            c = Case(torch, [70, 0], [39, 3], 40, 4, 2, 128, 16, dtype, True, seed=12, reach=reach)
+            c.scale = 0.0
+            c.check(torch)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [1, 7, 65, 140])
 def test_attention_sees_nothing(torch, rows, dtype):
     """Rows whose mask leaves nothing, with and without a context, and masks with bits past the rows."""
-    c = Case(torch, [0, 37, 0], [rows - 1] * 3, rows + 40, 4, 2, 128, 16, dtype, True, seed=5)
+    c = Case(torch, [0, 37, 0], [rows - 1] * 3, rows + 40, 4, 2, 128, 16, dtype, True, seed=5, reach=1500 * (rows % 3))
     c.mask[0, : rows // 2 + 1] = 0
     c.mask[1, ::2] = 0
     c.mask[:, :, (rows + 31) // 32:] = 0xFFFFFFFF  # nodes that do not exist
@@ -309,7 +332,7 @@ def test_attention_sees_nothing(torch, rows, dtype):
 def test_attention_not_a_number(torch, rows, dtype):
     """A stored not-a-number reaches the rows that see it and no other; bytes behind a request's last row
     (unwritten memory) reach none."""
-    c = Case(torch, [50, 21], [rows - 1] * 2, rows, 6, 2, 64, 32, dtype, True, seed=9)
+    c = Case(torch, [50, 21], [rows - 1] * 2, rows, 6, 2, 64, 32, dtype, True, seed=9, reach=17000 * (rows % 4 == 2))
     c.mask[:] = 0
     for i in range(rows):
         c.mask[:, i, i // 32] |= np.uint32(1 << (i % 32))
@@ -343,11 +366,11 @@ def test_attention_unwritten_bytes(torch):
         assert torch.equal(out[:, :rows], want[:, :rows])
 
 
-@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("rows", [1, 30, 70])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_without_pages(torch, rows, dtype):
     """Positions past the table and page ids that do not exist read as not-a-number, in the rows that see them."""
-    c = Case(torch, [100, 64, 10], [rows - 1] * 3, rows, 4, 1, 128, 16, dtype, False, seed=3)
+    c = Case(torch, [100, 64, 10], [rows - 1] * 3, rows, 4, 1, 128, 16, dtype, False, seed=3, reach=40 * rows)
     c.table[0, 2] = len(c.ref.k) // 16       # a page that does not exist
     c.table[1, (64 + rows - 1) // 16] = -1   # the last rows' page is missing
     out, _ = c.check(torch)
@@ -407,8 +430,14 @@ def test_attention_far_pages(torch):
 def test_attention_large_scores(torch):
     """Scores of some hundreds: weights that vanish, maxima that rise late, in an order of either kind."""
     for dtype in ("bf16", "f32"):
-        for rows in (1, 40):
-            c = Case(torch, [700], [rows - 1], rows, 4, 2, 128, 16, dtype, False, seed=8, kscale=12.0)
+        for rows in (1, 40, 70):
+            c = Case(torch, [700], [rows - 1], rows, 4, 2, 128, 16, dtype, False, seed=8, kscale=12.0, reach=17000 * (rows != 40))
+            c.check(torch)
+            # keys that grow along the context, so that every tile raises the maximum
+            c.ref.k *= np.exp2(np.minimum(np.arange(len(c.ref.k)) // 100, 6) - 6.0)[:, None, None]
+            c.check(torch)
+            c.q[:] = c.q.abs()
+            c.ref.k[:] = np.abs(c.ref.k)
             c.check(torch)
             c.scale = -c.scale
             c.check(torch)
