@@ -9,12 +9,15 @@
 //
 // Scores.  S^T = K Q^T on the scaled matrix instruction 16x16x128: its A operand
 // is the cache as it lies (16 tokens, 32 E2M1 codes and their scale byte a
-// lane), so keys are never unpacked.  Its B operand has 8 bits: a query is
-// scaled by a power of two to [128, 256) at its largest and cut into two E4M3
-// pieces of 4 significant bits each, the second holding what the first left, at
-// 2^-4 of its scale: together all 8 bits of a bf16.  That instruction drops up to
-// 2^-15 of the sum of a dot product's magnitudes, which an fp32 query would
-// show; fp32 queries take three bf16 pieces and keys unpacked to bf16 (exact).
+// lane), so keys are never unpacked.  Its B operand has 8 bits: a query is cut
+// into two E4M3 pieces of 4 significant bits, the second holding what the first
+// left.  Among eight products the instruction drops what is below about 2^-13 of
+// the largest, so the first piece has no more bits than that: scaled by a power of
+// two to [2, 4) at its largest, its quantum is 2^-9 (E4M3's least), and what is
+// smaller goes to the second piece, taken 2^7 times, whose quantum is then 2^-16.
+// The logarithms of sums come out 5e-8 to 1.6e-7 off, relative; with the largest
+// scaled to [128, 256) and the second piece taken 2^4 times, 1e-7 to 6e-7.
+// fp32 queries take three bf16 pieces and keys unpacked to bf16 (exact).
 //
 // Values.  O^T = V^T P^T on 16x16x32 bf16 (a value of the cache is exact in
 // bf16).  Values are unpacked once per workgroup into LDS, [token][element],
@@ -104,8 +107,8 @@ struct AttnQuery<S, false> {
         }
     top = max(top, (uint32_t)xor16_i32((int)top));
     top = max(top, (uint32_t)xor32_i32((int)top));
-    const int e = max((int)(top >> 23), 8);  // x * 2^(134 - e) has its largest in [128, 256)
-    const float up = (scale_log2 < 0.f ? -1.f : 1.f) * __uint_as_float((uint32_t)(261 - e) << 23);
+    const int e = max((int)(top >> 23), 2);  // x * 2^(128 - e) has its largest in [2, 4)
+    const float up = (scale_log2 < 0.f ? -1.f : 1.f) * __uint_as_float((uint32_t)(255 - e) << 23);
 #pragma unroll
     for (int k = 0; k < S::kKSteps; ++k)
 #pragma unroll
@@ -116,22 +119,22 @@ struct AttnQuery<S, false> {
         int word = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         word = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], word, true);
         w[k][0][u] = word;
-        y[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(word, 0)) * 16.f;
-        y[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(word, 1)) * 16.f;
-        y[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(word, 2)) * 16.f;
-        y[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(word, 3)) * 16.f;
+        y[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(word, 0)) * 128.f;
+        y[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(word, 1)) * 128.f;
+        y[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(word, 2)) * 128.f;
+        y[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(word, 3)) * 128.f;
         word = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         w[k][1][u] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], word, true);
       }
     // never 0, so that a hidden score's -inf stays one
-    return fmaxf(__builtin_fabsf(scale_log2) * __uint_as_float((uint32_t)max(e - 7, 1) << 23), 1e-36f);
+    return fmaxf(__builtin_fabsf(scale_log2) * __uint_as_float((uint32_t)max(e - 1, 1) << 23), 1e-36f);
   }
 
   // Product `i` of kProducts with 128 elements of 16 keys: small ones first.
   static constexpr int kProducts = 2;
   __device__ __forceinline__ f32x4 product(int i, i32x4 codes, int scale, int k, f32x4 acc) const {
     const i32x8 a = {codes[0], codes[1], codes[2], codes[3], 0, 0, 0, 0};
-    return i == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][1], acc, 4, 0, 0, scale, 0, 127 - 4)
+    return i == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][1], acc, 4, 0, 0, scale, 0, 127 - 7)
                   : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][0], acc, 4, 0, 0, scale, 0, 127);
   }
 };
