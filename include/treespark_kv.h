@@ -84,8 +84,8 @@ size_t ts_kv_block_bytes(int32_t page_size, int32_t head_dim);
  * in it, and a page id outside [0, num_pages) gives slot -1.  len, n and the
  * other arrays must not overlap.  Asynchronous on `stream`.  Host checks: null
  * pointers, 0 <= R <= 65536, 1 <= cap <= TS_KV_MAX_CAP, page_size, num_pages
- * >= 1 with num_pages * page_size < 2^31, max_blocks >= 1 with R * max_blocks,
- * R * cap < 2^31 and max_blocks * page_size <= 2^30.
+ * >= 1 with num_pages * page_size < 2^31, max_blocks >= 1 with R * max_blocks +
+ * num_pages, R * cap < 2^31 and max_blocks * page_size <= 2^30.
  */
 int32_t ts_kv_plan(const int32_t* len, const int32_t* n, int32_t R, int32_t cap, int32_t page_size,
                    int32_t num_pages, int32_t max_blocks, int32_t* free_pages, int32_t* free_count,
@@ -106,7 +106,7 @@ int32_t ts_kv_plan(const int32_t* len, const int32_t* n, int32_t R, int32_t cap,
  * a (row, head) holds a NaN or an infinity, all its key scales are 255 and its
  * values zero: rows that attend to it give NaN, others are not touched by it.
  * Asynchronous on `stream`.  Host checks: the cache, null pointers, layer,
- * dtype, rows >= 0, strides, alignment.
+ * dtype, rows >= 0 with rows * heads * head_dim <= 2^34, strides, alignment.
  */
 int32_t ts_kv_append(const ts_kv_cache* cache, int32_t layer, const void* k, const void* v, int32_t dtype,
                      int64_t k_stride, int64_t v_stride, const int32_t* slot, int32_t rows, void* stream);
@@ -142,22 +142,27 @@ size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32
  *      [0, num_pages) reads as not-a-number; nothing outside is read;
  *   mask: DEVICE [R][cap][ts_tree_mask_words(cap)] as ts_tree_mask writes it
  *      (bits past row n[q] do not count), or NULL;
- *   scale: finite (usually head_dim^-0.5);
+ *   scale: below 2^127 in magnitude (usually head_dim^-0.5);
  *   out: DEVICE [R][cap][q_heads][head_dim] of dtype, 16-byte aligned; lse (may
  *      be NULL): DEVICE float [R][cap][q_heads], log sum_t exp(scale <Q, K_t>).
- *      Rows past n[q] of both are left as they were.
- * Products of 4-bit keys with the queries, softmax statistics and sums are
- * held in fp32.  With TS_BF16 the weights w_t are rounded to bf16 before
- * they multiply the values (and the sum of weights is that of the rounded
- * ones); with TS_F32 nothing is rounded below fp32.
- * The result does not depend on what else the device runs: the same call
- * gives the same bits.  Asynchronous on `stream`; workspace: DEVICE, 16-byte
+ *      Rows past n[q] of both are left as they were.  Neither may overlap an
+ *      input.
+ * Scores, softmax statistics and sums are held in fp32.  With TS_F32 nothing is
+ * rounded below that.  With TS_BF16
+ *   - the matrix unit that multiplies 4-bit keys drops, among eight products at a
+ *     time, what is below about 2^-13 of the largest, and a query's elements are
+ *     held to 2^-18 of its head's largest: a score is off by at most
+ *     scale * (2^-15 sum |Q| |K_t| + 2^-18 max |Q| sum |K_t|), usually far less;
+ *   - a weight w_t is rounded to bf16 before it multiplies a value, and out is
+ *     divided by the sum of the rounded weights; lse is that of the unrounded ones.
+ * A call's result does not depend on what else the device runs: the same call on
+ * the same device gives the same bits.  Asynchronous on `stream`; workspace: DEVICE, 16-byte
  * aligned, of at least ts_kv_attention_workspace_size bytes, not shared by
  * calls that may overlap.
  * Host checks: the cache, null pointers, layer, dtype, q_heads a multiple of
- * heads, 0 <= R <= 65536, 1 <= cap <= TS_MAX_CAP (TS_KV_MAX_CAP without a
- * mask), R * cap * q_heads < 2^31, max_blocks, strides, alignment, scale,
- * workspace.
+ * heads and at most 256 times them, 0 <= R <= 65536, 1 <= cap <= TS_MAX_CAP
+ * (TS_KV_MAX_CAP without a mask), R * cap * q_heads < 2^31, max_blocks, strides,
+ * alignment, scale, out not q, workspace.
  */
 int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, int32_t dtype, int64_t q_stride,
                         int32_t q_heads, const int32_t* len, const int32_t* n, int32_t R, int32_t cap,
@@ -173,12 +178,12 @@ int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, 
  * back the pages it no longer needs.
  *   len, n [R], table [R][max_blocks], path_nodes [R][TS_MAX_D], path_len [R]:
  *      DEVICE (ts_verify's results, copied to the device); new_len [R]: DEVICE
- *      output, not the array len.
+ *      output, none of the inputs.
  * n[q] < 0 or path_len[q] < 0: the request keeps len[q].  A path stops before a
  * node that is not larger than the one before it, larger than n[q], or whose
  * place lies in no page; path_len[q] > TS_MAX_D is read as TS_MAX_D.
  * Asynchronous on `stream`.  Host checks: the cache, null pointers, 0 <= R <=
- * 65536, max_blocks, new_len != len.
+ * 65536, max_blocks, new_len.
  */
 int32_t ts_kv_accept(const ts_kv_cache* cache, const int32_t* len, const int32_t* n, int32_t R,
                      const int32_t* table, int32_t max_blocks, const int32_t* path_nodes,

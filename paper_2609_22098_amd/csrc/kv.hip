@@ -8,6 +8,8 @@ namespace ts {
 namespace {
 
 constexpr int kMaxRequests = 65536;
+constexpr int kMaxGroup = 256;  // (2^30 tokens of 256 heads) * 2^24 steps: places in the attention's line stay in 64 bits
+constexpr int64_t kMaxElements = (int64_t)1 << 34;  // of rows in one call: 2^31 threads
 
 bool page_size_ok(int32_t p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
 bool head_dim_ok(int32_t d) { return d == 64 || d == 128 || d == 256; }
@@ -148,6 +150,8 @@ int32_t ts_kv_plan(const int32_t* len, const int32_t* n, int32_t R, int32_t cap,
   if (num_pages < 1) return fail(TS_EINVAL, "num_pages=%d", num_pages);
   if ((int64_t)num_pages * page_size >= (int64_t)1 << 31)
     return fail(TS_EUNSUPPORTED, "num_pages * page_size = %lld reaches 2^31", (long long)num_pages * page_size);
+  if ((int64_t)R * max_blocks + num_pages >= (int64_t)1 << 31)
+    return fail(TS_EUNSUPPORTED, "R * max_blocks + num_pages = %lld reaches 2^31", (long long)R * max_blocks + num_pages);
   if (R == 0) return TS_OK;
   if (!len || !n || !free_pages || !free_count || !held || !table || !granted)
     return fail(TS_EINVAL, "a required array is NULL");
@@ -173,7 +177,8 @@ int32_t ts_kv_append(const ts_kv_cache* cache, int32_t layer, const void* k, con
     return fail(TS_EINVAL, "strides %lld, %lld: at least %lld elements and whole 16 bytes are needed", (long long)k_stride,
                 (long long)v_stride, (long long)width);
   if (!aligned16(k) || !aligned16(v)) return fail(TS_EINVAL, "k and v must start at 16-byte aligned addresses");
-  if ((int64_t)rows * width >= (int64_t)1 << 40) return fail(TS_EUNSUPPORTED, "rows=%d", rows);
+  if (rows * width > kMaxElements)
+    return fail(TS_EUNSUPPORTED, "rows * heads * head_dim = %lld exceeds 2^34", (long long)(rows * width));
   hipStream_t s = static_cast<hipStream_t>(stream);
   const KvAppendParams p = {view(cache, layer), k, v, k_stride, v_stride, slot, rows};
   launch_kv_append(p, cache->head_dim, dtype == TS_BF16, s);
@@ -191,7 +196,9 @@ int32_t ts_kv_read(const ts_kv_cache* cache, int32_t layer, int32_t layers, cons
   if (rows == 0 || (!k && !v)) return TS_OK;
   if (!slot) return fail(TS_EINVAL, "slot is NULL");
   if (!aligned16(k) || !aligned16(v)) return fail(TS_EINVAL, "k and v must start at 16-byte aligned addresses");
-  if ((int64_t)rows * cache->heads * cache->head_dim >= (int64_t)1 << 40) return fail(TS_EUNSUPPORTED, "rows=%d", rows);
+  const int64_t width = (int64_t)cache->heads * cache->head_dim;
+  if (rows * width > kMaxElements)
+    return fail(TS_EUNSUPPORTED, "rows * heads * head_dim = %lld exceeds 2^34", (long long)(rows * width));
   hipStream_t s = static_cast<hipStream_t>(stream);
   const KvReadParams p = {view(cache, layer), slot, rows, layers, k, v};
   launch_kv_read(p, cache->head_dim, dtype == TS_BF16, s);
@@ -202,7 +209,7 @@ int32_t ts_kv_read(const ts_kv_cache* cache, int32_t layer, int32_t layers, cons
 size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32_t cap, int32_t q_heads, int32_t dtype) {
   clear_error();
   if (check_cache(cache) || check_dtype(dtype) || R < 0 || R > kMaxRequests || cap < 1 || cap > TS_KV_MAX_CAP || q_heads < 1 ||
-      q_heads % cache->heads)
+      q_heads % cache->heads || q_heads / cache->heads > kMaxGroup)
     return 0;
   return attn_plan(cache, R, cap, q_heads, dtype, 0, compute_units()).bytes;
 }
@@ -218,11 +225,13 @@ int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, 
   TS_CHECK(check_requests(R, max_blocks, cache->page_size));
   if (q_heads < 1 || q_heads % cache->heads)
     return fail(TS_EINVAL, "q_heads=%d is no positive multiple of the cache's %d heads", q_heads, cache->heads);
+  if (q_heads / cache->heads > kMaxGroup)
+    return fail(TS_EUNSUPPORTED, "q_heads / heads = %d exceeds %d", q_heads / cache->heads, kMaxGroup);
   const int32_t most = mask ? TS_MAX_CAP : TS_KV_MAX_CAP;
   if (cap < 1 || cap > most) return fail(TS_EINVAL, "cap=%d outside [1, %d]", cap, most);
   if ((int64_t)R * cap * q_heads >= (int64_t)1 << 31)
     return fail(TS_EUNSUPPORTED, "R * cap * q_heads = %lld reaches 2^31", (long long)R * cap * q_heads);
-  if (!std::isfinite(scale)) return fail(TS_EINVAL, "scale must be finite");
+  if (!std::isfinite(scale * kLog2e)) return fail(TS_EINVAL, "scale must be finite and below 2^127");
   if (R == 0) return TS_OK;
   if (!q || !len || !n || !table || !out) return fail(TS_EINVAL, "a required array is NULL");
   const int64_t width = (int64_t)q_heads * cache->head_dim;
@@ -234,6 +243,7 @@ int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, 
   if (workspace_bytes < need) return fail(TS_ENOSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
   const AttnPlan plan = attn_plan(cache, R, cap, q_heads, dtype, (int64_t)max_blocks * cache->page_size, cus);
   if (!workspace || !aligned16(workspace)) return fail(TS_EINVAL, "workspace must be 16-byte aligned memory");
+  if (q == out) return fail(TS_EINVAL, "out must not be the array q");
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   const KvAttnParams p = {view(cache, layer), q, q_stride, q_heads, q_heads / cache->heads, R, cap, max_blocks,
@@ -256,7 +266,8 @@ int32_t ts_kv_accept(const ts_kv_cache* cache, const int32_t* len, const int32_t
   TS_CHECK(check_requests(R, max_blocks, cache->page_size));
   if (R == 0) return TS_OK;
   if (!len || !n || !table || !path_nodes || !path_len || !new_len) return fail(TS_EINVAL, "a required array is NULL");
-  if (new_len == len) return fail(TS_EINVAL, "new_len must not be the array len");
+  if (new_len == len || new_len == n || new_len == path_len)
+    return fail(TS_EINVAL, "new_len must not be one of the inputs");
   hipStream_t s = static_cast<hipStream_t>(stream);
   const KvAcceptParams p = {view(cache, 0), cache->layers, len, n, table, path_nodes, path_len, R, max_blocks, new_len};
   launch_kv_accept(p, cache->head_dim, s);

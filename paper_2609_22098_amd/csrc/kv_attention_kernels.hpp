@@ -471,7 +471,7 @@ void kv_attention_kernel(KvAttnParams p) {
       const bool there = m < rows_m;
       const int i = there ? m / g_rows : 0, g = there ? m - i * g_rows : 0;
       row_i[b] = there ? i : -1;
-      qp[b].fetch(static_cast<const TE*>(p.q) + ((int64_t)q * p.cap + i) * p.q_stride + (head * g_rows + g) * D, quarter);
+      qp[b].fetch(static_cast<const TE*>(p.q) + ((int64_t)q * p.cap + i) * p.q_stride + (int64_t)(head * g_rows + g) * D, quarter);
     }
     pages_of(s0, entry, pg[0]);
     load_keys(s0, pg[0]);
@@ -574,14 +574,18 @@ void kv_attention_kernel(KvAttnParams p) {
     // Weights of two runs as the products' B operand, and their sums: as they are
     // for the log-sum-exp, and as the products take them, which is what outputs are
     // divided by, so that the rounding of a row's large weights cancels.
-    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP], float (&sum)[MB], float (&rsum)[MB]) {
+    // `fused`: with one rounding instead of two.  The maximum was rounded when it was
+    // taken times c_row: a weight against it is then off by a factor of up to
+    // 2^(|m| 2^-24), the same for all of a row, which must not be large.
+    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP], float (&sum)[MB], float (&rsum)[MB], bool fused) {
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
         sum[b] = 0.f;
         rsum[b] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float left = exp2_fast(__builtin_fmaf(x[b][u0 + e / 4][e % 4], c_row[b], m_neg[b]));
+          float left = exp2_fast(fused ? __builtin_fmaf(x[b][u0 + e / 4][e % 4], c_row[b], m_neg[b])
+                                       : x[b][u0 + e / 4][e % 4] * c_row[b] + m_neg[b]);
           sum[b] += left;
 #pragma unroll
           for (int piece = 0; piece < S::kP; ++piece) {
@@ -649,7 +653,7 @@ void kv_attention_kernel(KvAttnParams p) {
             if (half == 1 && more) load_values(s + 1, pg[1]);
             bf16x8 w8[MB][S::kP];
             float sum[MB], rsum[MB];
-            weigh(sc, 2 * half, w8, sum, rsum);
+            weigh(sc, 2 * half, w8, sum, rsum, false);
 #pragma unroll
             for (int b = 0; b < MB; ++b) l_run[b] += sum[b], r_run[b] += rsum[b];
             wave_lds_sync();
@@ -672,7 +676,8 @@ void kv_attention_kernel(KvAttnParams p) {
       // see; elsewhere weights are taken against what there is, and only where a sum
       // of them passes kMost is the maximum found and the half weighed again.  (Any
       // reference serves as long as nothing overflows: fp32 sums and bf16 weights
-      // are as exact at 2^12 as at 1.)  Values lie in a ring of three tiles: the one that
+      // are as exact at 2^12 as at 1.)  Weights are taken with one fused operation (two:
+      // prompts of 8000 rows 695 us, this 650), but beyond scores of 2^22 with two.  Values lie in a ring of three tiles: the one that
       // is unpacked, the one at hand and the one whose second half is still due.
       constexpr int kSlot = 64 * S::kVRow;
       int cur = 0, before = 0;
@@ -704,7 +709,7 @@ void kv_attention_kernel(KvAttnParams p) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
         float sum[MB], rsum[MB];
-        constexpr float kMost = 4096.f;
+        constexpr float kMost = 4096.f, kFused = 4194304.f;  // 2^22
         auto raise = [&](auto& x, int u0, int t0, bool part) {
           if (part) hide(x, u0, t0);
           float top[MB];
@@ -720,10 +725,10 @@ void kv_attention_kernel(KvAttnParams p) {
         auto settle = [&](auto& x, int u0, int t0, bf16x8 (&w)[MB][S::kP]) {
           bool over = false;
 #pragma unroll
-          for (int b = 0; b < MB; ++b) over |= sum[b] > kMost;
+          for (int b = 0; b < MB; ++b) over |= sum[b] > kMost || __builtin_fabsf(m_neg[b]) > kFused;
           if (__any(over)) {
             raise(x, u0, t0, false);  // hidden already
-            weigh(x, 0, w, sum, rsum);
+            weigh(x, 0, w, sum, rsum, false);
           }
 #pragma unroll
           for (int b = 0; b < MB; ++b) l_run[b] += sum[b], r_run[b] += rsum[b];
@@ -756,7 +761,7 @@ void kv_attention_kernel(KvAttnParams p) {
           if (first) raise(sc[0], 0, t0, part);
           read_group(v_lds + cur, 0);
           score(sc[1], 2, pg[0]);
-          weigh(sc[0], 0, w8[0], sum, rsum);
+          weigh(sc[0], 0, w8[0], sum, rsum, true);
           stay(sc[1]);
           interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
           settle(sc[0], 0, t0, w8[0]);
@@ -774,7 +779,7 @@ void kv_attention_kernel(KvAttnParams p) {
           if (first) raise(sc[1], 2, t0, part);
           read_group(v_lds + cur + 32 * S::kVRow, 0);
           score(sc[0], 0, pg[1]);
-          weigh(sc[1], 0, w8[1], sum, rsum);
+          weigh(sc[1], 0, w8[1], sum, rsum, true);
           stay(sc[0]);
           interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
           settle(sc[1], 2, t0, w8[1]);

@@ -175,10 +175,16 @@ class Pool:
         elif any(t is None for t in given):
             raise ValueError("free_pages, free_count, held and table are given together")
         self.num_pages, self.R, self.max_blocks, self.page_size = num_pages, R, max_blocks, page_size
-        self.free_pages, self.free_count, self.held, self.table = free_pages, free_count, held, table
+        self._tensors = free_pages, free_count, held, table
         self.device = d = free_pages.get_device()
         self._addr = (_int32("free_pages", free_pages, (num_pages,), d), _int32("free_count", free_count, (1,), d),
                       _int32("held", held, (R,), d), _int32("table", table, (R, max_blocks), d))
+
+    # read-only: a plan goes by the tensors that the pool was made with
+    free_pages = property(lambda self: self._tensors[0])
+    free_count = property(lambda self: self._tensors[1])
+    held = property(lambda self: self._tensors[2])
+    table = property(lambda self: self._tensors[3])
 
 
 def plan(pool: Pool, length, n, cap, slots=True, out=None, stream=None):
@@ -209,10 +215,18 @@ def _rows(name, t, cache):
     heads, D = cache._row
     if len(sh) not in (3, 4) or sh[-1] != D or sh[-2] != heads or t.get_device() != cache.device:
         raise ValueError(f"{name}: [rows][{heads}][{D}] on cuda:{cache.device} is needed, got {list(sh)} on {t.device}")
-    if st[-1] != 1 or (st[-2] != D and heads > 1) or (len(sh) == 4 and st[0] != st[1] * sh[1] and sh[0] > 1):
-        raise ValueError(f"{name}: the heads of a row must be contiguous and rows evenly spaced, got strides {st}")
-    rows = sh[0] if len(sh) == 3 else sh[0] * sh[1]
-    return st[-3] if rows > 1 else max(st[-3], heads * D)
+    if st[-1] != 1 or (st[-2] != D and heads > 1):
+        raise ValueError(f"{name}: the heads of a row must be contiguous, got strides {st}")
+    return _row_stride(name, sh[:-2], st, heads * D)
+
+
+def _row_stride(name, sh, st, width):
+    """Elements from a row to the next of rows laid out as sh, [rows] or [R][cap]."""
+    if len(sh) == 2 and sh[1] > 1:
+        if sh[0] > 1 and st[0] != st[1] * sh[1]:
+            raise ValueError(f"{name}: rows must be evenly spaced, got strides {st}")
+        return st[1]
+    return st[0] if sh[0] > 1 else width
 
 
 def append(cache: Cache, k, v, slot, layer=0, stream=None):
@@ -281,8 +295,9 @@ def attention(cache: Cache, q, length, n, table, mask=None, scale=None, layer=0,
     if len(sh) != 4 or sh[3] != cache._row[1] or q.get_device() != d:
         raise ValueError(f"q: [R][cap][q_heads][{cache._row[1]}] on cuda:{d} is needed, got {list(sh)} on {q.device}")
     R, cap, q_heads, D = sh
-    if st[3] != 1 or (st[2] != D and q_heads > 1) or (st[0] != st[1] * cap and R > 1):
-        raise ValueError(f"q: the heads of a row must be contiguous and rows evenly spaced, got strides {st}")
+    if st[3] != 1 or (st[2] != D and q_heads > 1):
+        raise ValueError(f"q: the heads of a row must be contiguous, got strides {st}")
+    stride = _row_stride("q", sh[:2], st, q_heads * D)
     dtype = binding._dtype_code(q)
     if table.dim() != 2:
         raise ValueError("table: [R][max_blocks] is needed")
@@ -299,8 +314,8 @@ def attention(cache: Cache, q, length, n, table, mask=None, scale=None, layer=0,
                                 device=q.device)
     elif workspace.get_device() != d or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise ValueError(f"workspace: a contiguous uint8 tensor on cuda:{d} is needed")
-    _call(lib().ts_kv_attention, d, cache._ref, layer, q.data_ptr(), dtype,
-          st[1] if cap > 1 else st[0] if R > 1 else q_heads * D, q_heads, _int32("length", length, (R,), d),
+    _call(lib().ts_kv_attention, d, cache._ref, layer, q.data_ptr(), dtype, stride, q_heads,
+          _int32("length", length, (R,), d),
           _int32("n", n, (R,), d), R, cap, _int32("table", table, (R, max_blocks), d), max_blocks,
           None if mask is None else _int32("mask", mask, (R, cap, (cap + 31) // 32), d),
           D ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr() if lse is not None else None,

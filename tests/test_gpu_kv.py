@@ -405,6 +405,138 @@ def test_attention_strides(torch):
         assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_scores(torch, dtype, D):
+    """Queries whose elements lie 2^14 apart and whose rows lie 2^120 apart, on one token each: the log-sum-exp is then
+    the score itself.  Off by at most what the header states; in fp32 by D + 8 roundings of the sum of magnitudes."""
+    from paper_2609_22098_amd import kv
+    rng = np.random.default_rng(D)
+    R, hq, heads = 48, 6, 2
+    ref = kv_ref.Cache(R, 16, heads, D)
+    ref.k, ref.v = kv_ref.rounded(rng.standard_normal((R * 16, heads, D)) * 2.0 ** rng.integers(-20, 20, (R * 16, heads, 1)),
+                                  rng.standard_normal((R * 16, heads, D)))
+    cache = kv.Cache(torch.from_numpy(kv_ref.pack(ref, 1).copy()).cuda(), 16, heads, D)
+    q = rng.standard_normal((R, 1, hq, D)) * 2.0 ** rng.integers(-14, 1, (R, 1, hq, D)) * 2.0 ** rng.integers(-60, 60, (R, 1, hq, 1))
+    q[0] = 0
+    q[1] *= 2.0 ** -50
+    q[2, ..., :-1] = 0
+    q = torch.from_numpy(q).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    scale = 0.3
+    lse = torch.full((R, 1, hq), 99.0, device="cuda")
+    zero = _dev(torch, np.zeros(R))
+    out, _ = kv.attention(cache, q.cuda(), zero, zero, _dev(torch, np.arange(R)[:, None]), scale=scale, lse=lse)
+    x = q.double().numpy()[:, 0].reshape(R, heads, hq // heads, D)
+    k = ref.k[::16][:, :, None]
+    want = scale * (x * k).sum(-1).reshape(R, hq)
+    mag = np.abs(x * k).sum(-1)
+    if dtype == "bf16":
+        bound = 2.0 ** -15 * mag + 2.0 ** -18 * np.abs(x).max(-1) * np.abs(k).sum(-1)
+    else:
+        bound = (D + 8) * 2.0 ** -24 * mag
+    off = np.abs(lse.double().cpu().numpy()[:, 0] - want) - (scale * bound.reshape(R, hq) + 2.0 ** -22 * np.abs(want) + 1e-30)
+    assert off.max() <= 0, (off.max(), np.unravel_index(off.argmax(), off.shape))
+    value = np.broadcast_to(ref.v[::16][:, :, None], x.shape).reshape(R, 1, hq, D)  # a weight of 1 on one token
+    assert np.array_equal(out.double().cpu().numpy(), value)
+
+
+def test_attention_many_heads(torch):
+    """More elements in a row than 31 bits count (8 GiB of queries): the last heads' as those of a small call."""
+    from paper_2609_22098_amd import kv
+    heads, group, D = 65536, 256, 256
+    small = kv.empty_cache(1, 2, 16, 1, D)
+    x = torch.randn((11, 1, D), device="cuda")
+    slot = _dev(torch, np.arange(11))
+    kv.append(small, x, x.flip(0).contiguous(), slot)
+    block = kv.block_bytes(16, D)
+    pages = torch.zeros((1, 2, heads * block), dtype=torch.uint8, device="cuda")
+    pages[:, :, -block:] = small.pages
+    q = torch.zeros((1, 1, heads * group, D), dtype=torch.bfloat16, device="cuda")
+    q[:, :, -group:] = torch.randn((group, D), device="cuda").to(torch.bfloat16)
+    args = _dev(torch, [10]), _dev(torch, [0]), _dev(torch, [[0]])
+    want, _ = kv.attention(small, q[:, :, -group:].contiguous(), *args)
+    out, _ = kv.attention(kv.Cache(pages, 16, heads, D), q, *args)
+    # other tiles, so other references of the weights: each side off by half a step of outputs and of weights
+    off = (out[:, :, -group:].float() - want.float()).abs().max()
+    assert off <= 2 * (2.0 ** -8 + 2.0 ** -8) * x.abs().max() and want.abs().min(dim=-1).values.max() > 0
+    assert not out[:, :, : heads // 2].any()
+
+
+def test_rows_of_a_slice(torch):
+    """The last row of every request, as a slice leaves it: rows of one, far apart."""
+    from paper_2609_22098_amd import kv
+    R, cap, H, D = 3, 4, 2, 64
+    cache = kv.empty_cache(1, R, 16, H, D)
+    table = _dev(torch, np.arange(R)[:, None])
+    x = torch.randn((R, cap, 3 * H, D), device="cuda").to(torch.bfloat16)
+    last = x[:, -1:]
+    slot = _dev(torch, np.arange(R) * 16)
+    kv.append(cache, last[:, :, H: 2 * H], last[:, :, 2 * H:], slot)
+    k, v = kv.read(cache, slot)
+    zero = _dev(torch, np.zeros(R))
+    out, _ = kv.attention(cache, last[:, :, :H], zero, zero, table)
+    assert torch.equal(out[:, 0], v[0])
+    other = kv.empty_cache(1, R, 16, H, D)
+    kv.append(other, last[:, 0, H: 2 * H].contiguous(), last[:, 0, 2 * H:].contiguous(), slot)
+    assert torch.equal(other.pages, cache.pages)
+
+
+def test_binding_refusals(torch):
+    """Tensors of another type, shape, spacing or place raise before anything is launched."""
+    from paper_2609_22098_amd import kv
+    R, cap, H, D = 2, 3, 2, 64
+    pool = kv.Pool(6, R, 4, 16)
+    cache = kv.empty_cache(2, 6, 16, H, D)
+    length, n = _dev(torch, [5, 0]), _dev(torch, [2, 1])
+    slot, granted = kv.plan(pool, length, n, cap)
+    before = cache.pages.clone()
+    k = torch.randn((R * cap, H, D), device="cuda")
+    q = torch.randn((R, cap, 2 * H, D), device="cuda")
+    path, plen = _dev(torch, np.ones((R, 16))), _dev(torch, [1, 0])
+    bad = ValueError, TypeError, kv.TreeSparkError
+
+    for name in ("free_pages", "free_count", "held", "table"):
+        with pytest.raises(AttributeError):
+            setattr(pool, name, None)
+    for call in (
+            lambda: kv.Pool(6, R, 4, 16, held=pool.held), lambda: kv.Cache(cache.pages.float(), 16, H, D),
+            lambda: kv.Cache(cache.pages, 16, H + 1, D), lambda: kv.Cache(cache.pages, 20, H, D),
+            lambda: kv.Cache(cache.pages[..., ::2], 16, 1, D), lambda: kv.Cache(cache.pages[0], 16, H, D),
+            lambda: kv.plan(pool, length.long(), n, cap), lambda: kv.plan(pool, length, n[:1], cap),
+            lambda: kv.plan(pool, length.cpu(), n, cap), lambda: kv.plan(pool, length, n, 0),
+            lambda: kv.plan(pool, length, n, cap, out=(slot[:, :2], granted)),
+            lambda: kv.append(cache, k, k, slot.view(-1)[:5]), lambda: kv.append(cache, k, k.bfloat16(), slot),
+            lambda: kv.append(cache, k.half(), k.half(), slot), lambda: kv.append(cache, k[:, :1], k, slot),
+            lambda: kv.append(cache, k, k, slot.t()), lambda: kv.append(cache, k.cpu(), k.cpu(), slot),
+            lambda: kv.append(cache, k, k, slot, layer=2), lambda: kv.append(cache, k.transpose(1, 2), k, slot),
+            lambda: kv.append(cache, k.view(-1)[1:-127].view(-1, H, D), k[1:], slot.view(-1)[1:]),
+            lambda: kv.append(cache, k[::2].expand(2, 3, H, D), k.view(2, 3, H, D), slot),
+            lambda: kv.read(cache, slot.long()), lambda: kv.read(cache, slot, layer=1, layers=2),
+            lambda: kv.read(cache, slot, dtype=torch.float16), lambda: kv.read(cache, slot, layer=-1, layers=1),
+            lambda: kv.read(cache, slot, out=(torch.empty((1, 6, H, D), device="cuda"), None)),
+            lambda: kv.attention(cache, q.half(), length, granted, pool.table),
+            lambda: kv.attention(cache, q[..., :32], length, granted, pool.table),
+            lambda: kv.attention(cache, q[:, :, :3], length, granted, pool.table),
+            lambda: kv.attention(cache, q, length[:1], granted, pool.table),
+            lambda: kv.attention(cache, q, length, granted, pool.table[:, ::2]),
+            lambda: kv.attention(cache, q, length, granted, pool.table[0]),
+            lambda: kv.attention(cache, q[:, ::2], length, granted, pool.table),
+            lambda: kv.attention(cache, q, length, granted, pool.table, scale=float("nan")),
+            lambda: kv.attention(cache, q, length, granted, pool.table, out=q),
+            lambda: kv.attention(cache, q, length, granted, pool.table, out=torch.empty_like(q[:1])),
+            lambda: kv.attention(cache, q, length, granted, pool.table, lse=torch.empty((R, cap), device="cuda")),
+            lambda: kv.attention(cache, q, length, granted, pool.table, workspace=torch.empty(64, dtype=torch.uint8, device="cuda")),
+            lambda: kv.attention(cache, q, length, granted, pool.table, mask=torch.zeros((R, cap, 2), dtype=torch.int32, device="cuda")),
+            lambda: kv.accept(cache, length, granted, pool.table, path[:, :4], plen),
+            lambda: kv.accept(cache, length, granted, pool.table, path, plen, new_length=length),
+            lambda: kv.accept(cache, length, granted, pool.table, path, plen, new_length=granted),
+            lambda: kv.accept(cache, length, granted, pool.table, path.cpu(), plen)):
+        with pytest.raises(bad):
+            call()
+    torch.cuda.synchronize()
+    assert torch.equal(cache.pages, before) and pool.held.tolist() == [1, 1]
+
+
 def test_attention_far_pages(torch):
     """Pages whose offset passes 32 bits."""
     from paper_2609_22098_amd import kv
@@ -441,6 +573,28 @@ def test_attention_large_scores(torch):
             c.check(torch)
             c.scale = -c.scale
             c.check(torch)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,reach", [(1, 0), (1, 17000), (40, 0), (40, 17000), (300, 0)])
+def test_attention_one_hot(torch, rows, reach, dtype):
+    """Scores of 1e13, where fp32 steps by a million: the one token twice above the others has all the weight, early in
+    the context or behind keys that grow, and the outputs are its value."""
+    for star, grows in ((137, False), (599, True)):
+        c = Case(torch, [600], [rows - 1], rows, 4, 1, 128, 64, dtype, False, seed=rows, reach=reach)
+        token = np.full(len(c.ref.k), 2.0 ** -20)
+        pos = np.arange(600)
+        slot = c.table[0, pos // 64] * 64 + pos % 64
+        token[slot] = 2.0 ** (pos // 64 - 12) if grows else 1.0
+        token[slot[star]] = 4.0
+        c.ref.k = kv_ref.rounded(token[:, None, None] * np.ones_like(c.ref.k), c.ref.v)[0]
+        c.q[:] = c.q.abs() + 0.5
+        c.scale = 1e10
+        out, lse = c.run(torch)
+        want = np.broadcast_to(c.ref.v[slot[star], 0], out.shape)
+        assert np.array_equal(out.double().cpu().numpy(), want)
+        score = c.scale * 4.0 * c.q.double().sum(-1).numpy()
+        assert (np.abs(lse.double().cpu().numpy() - score) <= 2.0 ** -14 * score).all()
 
 
 # ---------------------------------------------------------------- accepted rows

@@ -100,6 +100,25 @@ def test_attention_refusals():
     assert _attention(c, R=0, q=None) == b.TS_OK
 
 
+def test_sizes_past_the_kernels_counters_are_refused():
+    """Groups whose places in the line of work could pass 64 bits, threads past a launch's 32, pages past 31; a scale
+    that is infinite in base 2; outputs on top of inputs."""
+    c = _cache()
+    assert _attention(c, hq=514, qs=514 * 128) == b.TS_EUNSUPPORTED
+    assert kv.lib().ts_kv_attention_workspace_size(ctypes.byref(c), 2, 5, 514, b.TS_BF16) == 0
+    assert kv.lib().ts_kv_attention_workspace_size(ctypes.byref(c), 2, 5, 512, b.TS_BF16) > 0
+    assert _attention(c, scale=3e38) == b.TS_EINVAL
+    assert _attention(c, q=FAKE, out=FAKE) == b.TS_EINVAL
+    big = _cache(heads=1024, head_dim=256, page_size=16, page_stride=1024 * 16 * 272)
+    big.layer_stride = 10 * big.page_stride
+    width = 1024 * 256
+    assert _append(big, ks=width, vs=width, rows=(1 << 16) + 1) == b.TS_EUNSUPPORTED
+    assert _read(big, rows=(1 << 16) + 1) == b.TS_EUNSUPPORTED
+    for same in ("n", "plen"):
+        assert _accept(c, **{same: FAKE + 64}) == b.TS_EINVAL
+    assert kv.lib().ts_kv_plan(FAKE, FAKE, 65536, 1, 16, (1 << 27) - 1, (1 << 15) - 1, *[FAKE] * 6, None) == b.TS_EUNSUPPORTED
+
+
 def test_attention_workspace():
     """A function of sizes alone, which a call refuses to go below; 0 for what it would refuse."""
     c, L = _cache(), kv.lib()
