@@ -67,7 +67,7 @@ KvView view(const ts_kv_cache* c, int32_t layer) {
 // their partial results lie in the workspace.
 struct AttnPlan {
   AttnTile tile;
-  int rows, groups, min_tokens, whole_tiles;
+  int rows, groups, min_tokens, spare, whole_tiles;
   size_t stats, joins, bytes;  // offsets after the parts, and all
 };
 
@@ -101,6 +101,7 @@ AttnPlan attn_plan(const ts_kv_cache* c, int32_t R, int32_t cap, int32_t q_heads
   // less than cutting and joining: nothing is cut.
   const int64_t tiles = (rows + x.rows - 1) / x.rows, all = tiles * c->heads * R;
   x.whole_tiles = tokens > 0 && tokens <= 1024 && all < 1 << 24 && (small || all >= cus) ? (int)tiles : 0;
+  x.spare = !x.whole_tiles && all * 4 <= x.groups ? (int)all : 0;
   const size_t parts = (size_t)x.groups * 2 * x.rows;
   x.stats = parts * c->head_dim * sizeof(float);
   x.joins = x.stats + parts * sizeof(AttnStat);
@@ -247,7 +248,7 @@ int32_t ts_kv_attention(const ts_kv_cache* cache, int32_t layer, const void* q, 
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   const KvAttnParams p = {view(cache, layer), q, q_stride, q_heads, q_heads / cache->heads, R, cap, max_blocks,
-                          ts_tree_mask_words(cap), len, n, table, mask, scale * kLog2e, out, lse, plan.min_tokens, plan.whole_tiles,
+                          ts_tree_mask_words(cap), len, n, table, mask, scale * kLog2e, out, lse, plan.min_tokens, plan.spare, plan.whole_tiles,
                           reinterpret_cast<float*>(ws), reinterpret_cast<AttnStat*>(ws + plan.stats),
                           reinterpret_cast<AttnJoin*>(ws + plan.joins)};
   const bool bf16 = dtype == TS_BF16;

@@ -197,6 +197,18 @@ struct AttnReq {
     first = (int64_t)(len + S::kFixed) * p.group + (p.mask ? rows * p.group : S::kRows);
     all = before(tiles);
   }
+  // All tiles as long as the longest.
+  __device__ __forceinline__ void level() {
+    first += more * (tiles - 1);
+    more = 0;
+    all = tiles * first;
+  }
+  // All tiles as long as the longest, up to whole pieces of `per`.
+  __device__ __forceinline__ void pad(int64_t per) {
+    level();
+    first = (first + per - 1) / per * per;
+    all = tiles * first;
+  }
   // sum over the tiles before tile t
   __device__ __forceinline__ int64_t before(int t) const { return t * first + more * ((int64_t)t * (t - 1) / 2); }
   // the tile that holds place x < all
@@ -271,8 +283,14 @@ void kv_attention_kernel(KvAttnParams p) {
   const int groups = gridDim.x, per_xcd = groups / 8;
   const int w = (int)blockIdx.x < per_xcd * 8 ? (blockIdx.x % 8) * per_xcd + blockIdx.x / 8 : blockIdx.x;
   // Inclusive sum over a thread's request and those before it from q0 on.
+  int64_t per = 0;  // length of a piece
   auto scan = [&](int q0, int64_t& v, int64_t& all) {
-    v = q0 + tid < p.R ? AttnReq<S>(p, q0 + tid).all * p.c.heads : 0;
+    v = 0;
+    if (q0 + tid < p.R) {
+      AttnReq<S> r(p, q0 + tid);
+      if (p.spare) per ? r.pad(per) : r.level();
+      v = r.all * p.c.heads;
+    }
     int64_t incl = v;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -291,7 +309,7 @@ void kv_attention_kernel(KvAttnParams p) {
     return incl;
   };
   int q;
-  int64_t at, begin, end, per;  // of request q's first step; the piece and every piece's length
+  int64_t at, begin, end;  // of request q's first step; the piece
   if (p.whole_tiles) {
     // short contexts: a tile a workgroup (of whole_tiles for each request and kv head)
     q = w / (p.c.heads * p.whole_tiles);
@@ -306,7 +324,15 @@ void kv_attention_kernel(KvAttnParams p) {
       scan(q0, v, all);
       total += all;
     }
-    per = max((total + groups - 1) / groups, (int64_t)p.min_tokens * p.group);
+    per = max((total + groups - p.spare - 1) / (groups - p.spare), (int64_t)p.min_tokens * p.group);
+    if (p.spare) {
+      // few tiles: each is padded to whole pieces, so that a workgroup has part of one
+      total = 0;
+      for (int q0 = 0; q0 < p.R; q0 += S::kThreads) {
+        incl = scan(q0, v, all);
+        total += all;
+      }
+    }
     begin = per * w, end = min(begin + per, total);
     if (tid == 0) p.joins[w].q = -1;
     if (begin >= end) return;
@@ -326,7 +352,8 @@ void kv_attention_kernel(KvAttnParams p) {
 
   const int g_rows = p.group;
   for (int64_t pos = begin; pos < end && q < p.R;) {
-    const AttnReq<S> r(p, q);
+    AttnReq<S> r(p, q);
+    if (p.spare) r.pad(per);
     if (pos >= at + r.all * p.c.heads) {
       at += r.all * p.c.heads;
       ++q;

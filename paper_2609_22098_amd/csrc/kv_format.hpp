@@ -146,6 +146,7 @@ struct KvAttnParams {
   void* out;
   float* lse;
   int min_tokens;  // of a workgroup's piece
+  int spare;       // workgroups left over for padding tiles to whole pieces; 0: no padding
   int whole_tiles; // tiles of a request and kv head, one a workgroup; 0: cut pieces
   float* parts;    // [2 * workgroups][rows of a tile][D]
   AttnStat* stats; // [2 * workgroups][rows of a tile]
