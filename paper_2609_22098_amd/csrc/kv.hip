@@ -79,7 +79,7 @@ struct AttnPlan {
 // trees of up to 65 rows and 4 query heads a kv head over 500 to 8000 tokens: tiles
 // of 128 rows 192 us, of 32 257, of 16 304).  A few tiles cut into many pieces
 // cost more in partial results than they gain, unless their context is long: one
-// such tree over 5003 tokens takes 40 us in tiles of 128 and 34 in tiles of 32,
+// such tree over 5003 tokens took 40 us in tiles of 128 and 34 in tiles of 32,
 // three of 33 rows in fp32 over 50 to 700 27 us in tiles of 64 and 21 in tiles of 16.
 //
 // The workgroups: what a compute unit holds of them, so that none waits.  Tiles of
@@ -97,10 +97,18 @@ AttnPlan attn_plan(const ts_kv_cache* c, int32_t R, int32_t cap, int32_t q_heads
   const bool small = x.tile == AttnTile::k16 || x.tile == AttnTile::k32;
   x.groups = cus * (c->head_dim == 256 ? 1 : x.tile == AttnTile::k16 && dtype == TS_BF16 && !few ? 3 : 2);
   x.min_tokens = small ? 256 : 64;  // a step
-  // Four steps of small tiles, sixteen of large ones that fill the device, take
-  // less than cutting and joining: nothing is cut.
+  // Four steps of small tiles, six of tiles of 32 that have a compute unit each,
+  // sixteen of large ones that fill the device, take less than cutting and joining:
+  // nothing is cut (a tree of 65 rows over 1100 tokens: 17 us, cut 21; over 2000:
+  // 23.5 and 23.6; one of 17 rows over 2000: 22 and 18; one row over 1100: 12.6 and
+  // 12.9, over 2000 17 and 13).
   const int64_t tiles = (rows + x.rows - 1) / x.rows, all = tiles * c->heads * R;
-  x.whole_tiles = tokens > 0 && tokens <= 1024 && all < 1 << 24 && (small || all >= cus) ? (int)tiles : 0;
+  const int64_t uncut = x.tile == AttnTile::k32 && all <= cus ? 1536 : 1024;
+  x.whole_tiles = tokens > 0 && tokens <= uncut && all < 1 << 24 && (small || all >= cus) ? (int)tiles : 0;
+  // Few tiles are padded to whole pieces: a workgroup that ends one tile and begins
+  // another pays for both (a tree of 65 rows over 5003 tokens, 72 tiles on 512
+  // workgroups: 34.8 us, padded 29.7; three of 33 rows over 500 to 2500, 120 tiles:
+  // 34 and 24). Padding costs up to a piece a tile, a quarter of all at the most.
   x.spare = !x.whole_tiles && all * 4 <= x.groups ? (int)all : 0;
   const size_t parts = (size_t)x.groups * 2 * x.rows;
   x.stats = parts * c->head_dim * sizeof(float);

@@ -278,10 +278,14 @@ void kv_attention_kernel(KvAttnParams p) {
   const int col = lane & 15, quarter = lane >> 4;
   const int shift = p.c.page_shift, in_page = (1 << shift) - 1;
 
-  // The workgroup's piece of the line: workgroups of one XCD (every eighth)
-  // take neighbouring pieces, so that row tiles of one request share its L2.
-  const int groups = gridDim.x, per_xcd = groups / 8;
-  const int w = (int)blockIdx.x < per_xcd * 8 ? (blockIdx.x % 8) * per_xcd + blockIdx.x / 8 : blockIdx.x;
+  // Of `pieces` of the line, the workgroup's: workgroups of one XCD (every eighth)
+  // take neighbouring ones, so that row tiles of one request share its L2.
+  const int groups = gridDim.x;
+  auto own = [&](int pieces) {
+    const int b = blockIdx.x, per_xcd = pieces / 8;
+    return b < per_xcd * 8 ? (b % 8) * per_xcd + b / 8 : b;
+  };
+  int w;
   // Inclusive sum over a thread's request and those before it from q0 on.
   int64_t per = 0;  // length of a piece
   auto scan = [&](int q0, int64_t& v, int64_t& all) {
@@ -312,6 +316,7 @@ void kv_attention_kernel(KvAttnParams p) {
   int64_t at, begin, end;  // of request q's first step; the piece
   if (p.whole_tiles) {
     // short contexts: a tile a workgroup (of whole_tiles for each request and kv head)
+    w = own(groups);
     q = w / (p.c.heads * p.whole_tiles);
     const int head = w / p.whole_tiles % p.c.heads, rt = w % p.whole_tiles;
     const AttnReq<S> r(p, q);
@@ -324,7 +329,13 @@ void kv_attention_kernel(KvAttnParams p) {
       scan(q0, v, all);
       total += all;
     }
-    per = max((total + groups - p.spare - 1) / (groups - p.spare), (int64_t)p.min_tokens * p.group);
+    const int64_t least = (int64_t)p.min_tokens * p.group;
+    auto piece = [&](int n) { return (total + n - 1) / n; };  // of n
+    per = piece(groups - p.spare);
+    // few tiles of few steps: one workgroup a compute unit (fp32, 20000 tokens of one
+    // row: 24.5 us with two, 21.2 with one; at eight steps a piece 38 and 42)
+    if (S::kResident > 1 && p.spare && 2 * per < 5 * least) per = piece(groups / 2 - p.spare);
+    per = max(per, least);
     if (p.spare) {
       // few tiles: each is padded to whole pieces, so that a workgroup has part of one
       total = 0;
@@ -333,6 +344,7 @@ void kv_attention_kernel(KvAttnParams p) {
         total += all;
       }
     }
+    w = own((int)((total + per - 1) / per));
     begin = per * w, end = min(begin + per, total);
     if (tid == 0) p.joins[w].q = -1;
     if (begin >= end) return;
