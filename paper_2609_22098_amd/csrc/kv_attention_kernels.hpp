@@ -29,7 +29,15 @@
 // Work.  The steps of all tiles of all requests, in one line, are cut into
 // equal pieces, one a workgroup: no length decides the balance.  A tile
 // that a cut goes through leaves partial results, and a second kernel joins them.
-// Where a table names few tokens, nothing is cut: a workgroup takes a tile.
+// Where there are few tiles, each is padded to whole pieces; where a table names
+// few tokens, nothing is cut: a workgroup takes a tile.
+//
+// Bounds.  Tiles of 16 rows: bytes (128 requests of one row over 300 to 16000
+// tokens, 557 MB: 116 us, 4.8 TB/s; 131001 tokens of one: 31 us, 4.6 TB/s).  Tiles of
+// 128: matrix and vector issue (prompts of 8000 rows over 2000 to 8000 tokens, 675
+// GFLOP: 630 us and 20 for the join, 1.03 PFLOP/s; 64 trees over 500 to 8000: 171 us
+// and 18).  Few short contexts: round trips (a tree of 65 rows over 5003 tokens: 23 us
+// and 7, of which 8 are steps).
 #pragma once
 
 #include "kv_format.hpp"
@@ -61,7 +69,7 @@ struct AttnShape {
   static constexpr int kORow = D + 4;            // floats of a row of results in LDS
   static constexpr int kVBytes = WT * kVTokens * kVRow;
   static constexpr int kOBytes = WT * WM * 16 * kORow * 4;
-  static constexpr int kFixed = 512;             // tokens' worth of a tile's beginning and end (128: 64 trees 222 us, this 198)
+  static constexpr int kFixed = 512;             // tokens' worth of a tile's beginning and end (128: 64 trees 220 us, 128 single rows 147; this 190 and 124)
   // workgroups on a compute unit: registers allow waves of 128 where a wave has one block of rows
   static constexpr int kResident = MB == 1 && D <= 128 && !kF32 ? 3 : D <= 128 ? 2 : 1;
   static constexpr int kLds = kVBytes > kOBytes ? kVBytes : kOBytes;
@@ -783,8 +791,8 @@ void kv_attention_kernel(KvAttnParams p) {
           look_up(s + 3, entry);
           const bool first = part || s == s0;
           // Two workgroups share a compute unit, and the older one's waves always go
-          // first: it ends at 580 us where the other needs 740.  They take turns at a
-          // higher priority instead, 41 us each by the device's clock.
+          // first: it ended at 580 us where the other needed 740.  They take turns at a
+          // higher priority instead, 41 us each by the device's clock (prompts of 8000 rows: 690 us, in turn 650).
           if ((uint32_t)__builtin_readsteadycounter() >> 12 & 1 ^ (blockIdx.x >= gridDim.x / 2)) __builtin_amdgcn_s_setprio(1);
           else __builtin_amdgcn_s_setprio(0);
           // What is loaded past the last tile lies in some page and is of no use; a

