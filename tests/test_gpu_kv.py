@@ -776,3 +776,47 @@ def test_round_in_a_graph(torch):
         assert torch.equal(caches[0].pages, caches[1].pages) and torch.equal(pools[0].table, pools[1].table)
         length = length + 1 + plen + (37 * r if r < 2 else 0)  # some contexts jump ahead, over rows never written
         assert outs[0].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_at_once_and_a_shared_workspace(torch, dtype):
+    """Calls in flight on two streams, each with a workspace; two captured graphs of other sizes that share one and are
+    replayed in turn: the bits of the same calls alone."""
+    from paper_2609_22098_amd import kv
+    calls = []
+    for seed, (lens, n, cap, hq, heads, page, reach) in enumerate([
+            ([7000, 2100], [16, 3], 17, 8, 2, 64, 0), ([3000] * 20, [64] * 20, 65, 8, 2, 16, 4000)]):
+        c = Case(torch, lens, n, cap, hq, heads, 128, page, dtype, True, seed=seed, reach=reach)
+        want, _ = c.run(torch)
+        cache = kv.Cache(torch.from_numpy(kv_ref.pack(c.ref, 1).copy()).cuda(), page, heads, 128)
+        args = [_dev(torch, a) for a in (c.lens, c.ns, c.table)]
+        kw = dict(mask=torch.from_numpy(c.mask.view(np.int32)).cuda(), scale=c.scale)
+        size = kv.attention_workspace_size(cache, len(lens), cap, hq, c.t)
+        calls.append((cache, c.q.cuda(), args, kw, want, size))
+    streams = [torch.cuda.Stream() for _ in calls]
+    own = [torch.empty(size, dtype=torch.uint8, device="cuda") for *_, size in calls]
+    outs = [[torch.full_like(want, 99.0) for _ in range(6)] for *_, want, _ in calls]
+    torch.cuda.synchronize()
+    for r in range(6):
+        for i, (cache, q, args, kw, _, _) in enumerate(calls):
+            kv.attention(cache, q, *args, out=outs[i][r], workspace=own[i], stream=streams[i], **kw)
+    torch.cuda.synchronize()
+    for i, (*_, want, _) in enumerate(calls):
+        assert all(torch.equal(o, want) for o in outs[i])
+
+    shared = torch.empty(max(size for *_, size in calls), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for cache, q, args, kw, want, _ in calls:
+        out, graph = torch.full_like(want, 99.0), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=streams[0]):
+            kv.attention(cache, q, *args, out=out, workspace=shared, **kw)
+        graphs.append(graph)
+        outs.append(out)
+    for r in range(4):
+        for i in (0, 1, 0) if r % 2 else (1, 0):
+            outs[i].fill_(99.0)
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for i, (*_, want, _) in enumerate(calls):
+            assert torch.equal(outs[i], want)
