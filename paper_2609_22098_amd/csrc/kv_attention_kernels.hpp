@@ -188,6 +188,11 @@ struct AttnQuery<S, true> {
   }
 };
 
+template <int N>
+struct Blocks {
+  static constexpr int value = N;
+};
+
 // One request's part in the line.  A row tile's length in it is the number of
 // (token, query head of the group) pairs that its last row may see, and as much
 // again as its beginning and end cost: with a mask the same for all tiles; a
@@ -514,7 +519,7 @@ void kv_attention_kernel(KvAttnParams p) {
     int row_i[MB];
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
-      const int m = m0 + (wm * MB + b) * 16 + col;
+      const int m = m0 + (b * WM + wm) * 16 + col;
       const bool there = m < rows_m;
       const int i = there ? m / g_rows : 0, g = there ? m - i * g_rows : 0;
       row_i[b] = there ? i : -1;
@@ -536,9 +541,9 @@ void kv_attention_kernel(KvAttnParams p) {
     constexpr int kGroups = D / 64;  // of four blocks of 16 elements
     // Scores of runs u0... of the keys in registers, on the pages `pg`.
     auto score = [&](auto& x, int u0, const int (&pg_)[kRuns]) {
-      constexpr int N = sizeof(x[0]) / sizeof(x[0][0]);
+      constexpr int NB = sizeof(x) / sizeof(x[0]), N = sizeof(x[0]) / sizeof(x[0][0]);
 #pragma unroll
-      for (int b = 0; b < MB; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int u = 0; u < N; ++u) x[b][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -551,14 +556,14 @@ void kv_attention_kernel(KvAttnParams p) {
             if (D < 128 && quarter >= 2) codes = i32x4{0, 0, 0, 0};
             const int scale = pg_[kRuns == 1 ? 0 : u0 + u] < 0 ? 255 : ks[u0 + u][k];
 #pragma unroll
-            for (int b = 0; b < MB; ++b) x[b][u] = qp[b].product(i, codes, scale, k, x[b][u]);
+            for (int b = 0; b < NB; ++b) x[b][u] = qp[b].product(i, codes, scale, k, x[b][u]);
           }
     };
     // -inf for what a row does not see, of runs u0... of the tile at t0.
     auto hide = [&](auto& x, int u0, int t0) {
-      constexpr int N = sizeof(x[0]) / sizeof(x[0][0]);
+      constexpr int NB = sizeof(x) / sizeof(x[0]), N = sizeof(x[0]) / sizeof(x[0][0]);
 #pragma unroll
-      for (int b = 0; b < MB; ++b) {
+      for (int b = 0; b < NB; ++b) {
         uint64_t sees = 0;
         const int i = row_i[b], j0 = t0 - context;
         if (i >= 0) {
@@ -586,10 +591,10 @@ void kv_attention_kernel(KvAttnParams p) {
         }
       }
     };
-    auto highest = [&](const auto& x, float (&top)[MB]) {
-      constexpr int N = sizeof(x[0]) / sizeof(x[0][0]);
+    auto highest = [&](const auto& x, auto& top) {
+      constexpr int NB = sizeof(x) / sizeof(x[0]), N = sizeof(x[0]) / sizeof(x[0][0]);
 #pragma unroll
-      for (int b = 0; b < MB; ++b) {
+      for (int b = 0; b < NB; ++b) {
         top[b] = kNegInf;
 #pragma unroll
         for (int u = 0; u < N; ++u)
@@ -601,13 +606,14 @@ void kv_attention_kernel(KvAttnParams p) {
     };
     // Raises what weights are taken against to the maximum `top`, which it may lag
     // behind by 2^8, so that most tiles rescale nothing.
-    auto rescale = [&](const float (&top)[MB]) {
+    auto rescale = [&](const auto& top) {
+      constexpr int NB = sizeof(top) / sizeof(top[0]);
       bool rises = false;
 #pragma unroll
-      for (int b = 0; b < MB; ++b) rises |= top[b] > m_run[b] + 8.f;
+      for (int b = 0; b < NB; ++b) rises |= top[b] > m_run[b] + 8.f;
       if (__any(rises))
 #pragma unroll
-        for (int b = 0; b < MB; ++b) {
+        for (int b = 0; b < NB; ++b) {
           const float m_new = fmaxf(m_run[b], top[b]);
           const float keep = m_new == kNegInf ? 1.f : exp2_fast(m_run[b] - m_new);
           m_run[b] = m_new;
@@ -624,9 +630,10 @@ void kv_attention_kernel(KvAttnParams p) {
     // `fused`: with one rounding instead of two.  The maximum was rounded when it was
     // taken times c_row: a weight against it is then off by a factor of up to
     // 2^(|m| 2^-24), the same for all of a row, which must not be large.
-    auto weigh = [&](const auto& x, int u0, bf16x8 (&w8)[MB][S::kP], float (&sum)[MB], float (&rsum)[MB], bool fused) {
+    auto weigh = [&](const auto& x, int u0, auto& w8, auto& sum, auto& rsum, bool fused) {
+      constexpr int NB = sizeof(x) / sizeof(x[0]);
 #pragma unroll
-      for (int b = 0; b < MB; ++b) {
+      for (int b = 0; b < NB; ++b) {
         sum[b] = 0.f;
         rsum[b] = 0.f;
 #pragma unroll
@@ -667,11 +674,12 @@ void kv_attention_kernel(KvAttnParams p) {
         va[g & 1][x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
     };
-    auto add_group = [&](int g, const bf16x8 (&w8)[MB][S::kP]) {
+    auto add_group = [&](int g, const auto& w8) {
+      constexpr int NB = sizeof(w8) / sizeof(w8[0]);
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int b = 0; b < MB; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int piece = S::kP - 1; piece >= 0; --piece)
             o[b][4 * g + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[g & 1][x]), w8[b][piece],
@@ -731,7 +739,7 @@ void kv_attention_kernel(KvAttnParams p) {
 #pragma unroll
       for (int j = 0; j < kVMine; ++j) unpack(j, pg[0], v_lds, 0);
       load_values(s0 + 1, pg[1]);
-      if (m0 + wm * MB * 16 >= rows_m) {
+      if (m0 + wm * 16 >= rows_m) {
         // no rows for this wave: it unpacks its share of the values
         __syncthreads();
         for (int s = s0; s < s1; ++s) {
@@ -747,100 +755,106 @@ void kv_attention_kernel(KvAttnParams p) {
           for (int u = 0; u < kRuns; ++u) pg[1][u] = pg[2][u];
         }
       } else {
-        f32x4 sc[2][MB][2];
-        bf16x8 w8[2][MB][S::kP];
-#pragma unroll
-        for (int b = 0; b < MB; ++b)
-#pragma unroll
-          for (int piece = 0; piece < S::kP; ++piece)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
-        float sum[MB], rsum[MB];
-        constexpr float kMost = 4096.f, kFused = 4194304.f;  // 2^22
-        auto raise = [&](auto& x, int u0, int t0, bool part) {
-          if (part) hide(x, u0, t0);
-          float top[MB];
-          highest(x, top);
-          rescale(top);
-        };
-        // The products are issued before this point, not behind the branch that follows
-        // (no instruction: nothing waits for their results).
-        auto stay = [&](f32x4 (&x)[MB][2]) {
-#pragma unroll
-          for (int b = 0; b < MB; ++b) asm volatile("" : "+v"(x[b][0]), "+v"(x[b][1]));
-        };
-        auto settle = [&](auto& x, int u0, int t0, bf16x8 (&w)[MB][S::kP]) {
-          bool over = false;
-#pragma unroll
-          for (int b = 0; b < MB; ++b) over |= sum[b] > kMost || __builtin_fabsf(m_neg[b]) > kFused;
-          if (__any(over)) {
-            raise(x, u0, t0, false);  // hidden already
-            weigh(x, 0, w, sum, rsum, false);
+        // with the blocks of 16 rows that the wave has
+        auto run = [&](auto blocks) {
+          constexpr int NB = decltype(blocks)::value;
+          f32x4 sc[2][NB][2];
+          bf16x8 w8[2][NB][S::kP];
+  #pragma unroll
+          for (int b = 0; b < NB; ++b)
+  #pragma unroll
+            for (int piece = 0; piece < S::kP; ++piece)
+  #pragma unroll
+              for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
+          float sum[NB], rsum[NB];
+          constexpr float kMost = 4096.f, kFused = 4194304.f;  // 2^22
+          auto raise = [&](auto& x, int u0, int t0, bool part) {
+            if (part) hide(x, u0, t0);
+            float top[NB];
+            highest(x, top);
+            rescale(top);
+          };
+          // The products are issued before this point, not behind the branch that follows
+          // (no instruction: nothing waits for their results).
+          auto stay = [&](f32x4 (&x)[NB][2]) {
+  #pragma unroll
+            for (int b = 0; b < NB; ++b) asm volatile("" : "+v"(x[b][0]), "+v"(x[b][1]));
+          };
+          auto settle = [&](auto& x, int u0, int t0, bf16x8 (&w)[NB][S::kP]) {
+            bool over = false;
+  #pragma unroll
+            for (int b = 0; b < NB; ++b) over |= sum[b] > kMost || __builtin_fabsf(m_neg[b]) > kFused;
+            if (__any(over)) {
+              raise(x, u0, t0, false);  // hidden already
+              weigh(x, 0, w, sum, rsum, false);
+            }
+  #pragma unroll
+            for (int b = 0; b < NB; ++b) l_run[b] += sum[b], r_run[b] += rsum[b];
+          };
+          score(sc[0], 0, pg[0]);
+          __syncthreads();
+          read_group(v_lds + 32 * S::kVRow, 0);  // multiplied with weights of zero
+          for (int s = s0; s < s1; ++s) {
+            const int t0 = (s * WT + wt) * S::kTile;
+            const bool part = t0 + S::kTile > all_seen;
+            const int next = cur == 2 * kSlot ? 0 : cur + kSlot;
+            pages_of(s + 2, entry, pg[2]);
+            look_up(s + 3, entry);
+            const bool first = part || s == s0;
+            // Two workgroups share a compute unit, and the older one's waves always go
+            // first: it ended at 580 us where the other needed 740.  They take turns at a
+            // higher priority instead, 41 us each by the device's clock (prompts of 8000 rows: 690 us, in turn 650).
+            if ((uint32_t)__builtin_readsteadycounter() >> 12 & 1 ^ (blockIdx.x >= gridDim.x / 2)) __builtin_amdgcn_s_setprio(1);
+            else __builtin_amdgcn_s_setprio(0);
+            // What is loaded past the last tile lies in some page and is of no use; a
+            // branch around it would keep the products from running beside the rest.
+            // second half of the tile before, first half's weights, second half's scores
+            load_keys(s + 1, pg[1], 0);
+  #pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+              if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
+              add_group(g, w8[1]);
+            }
+            interleave<NB * S::kP * D / 16, 2>();
+            if (first) raise(sc[0], 0, t0, part);
+            read_group(v_lds + cur, 0);
+            score(sc[1], 2, pg[0]);
+            weigh(sc[0], 0, w8[0], sum, rsum, true);
+            stay(sc[1]);
+            interleave<NB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
+            settle(sc[0], 0, t0, w8[0]);
+            // first half of this tile, second half's weights, the next tile's scores
+            load_keys(s + 1, pg[1], 2);
+  #pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+              if (g + 1 < kGroups) read_group(v_lds + cur, g + 1);
+              add_group(g, w8[0]);
+            }
+  #pragma unroll
+            for (int j = 0; j < kVMine; ++j) unpack(j, pg[1], v_lds + next, 0);
+            load_values(s + 2, pg[2]);
+            interleave<NB * S::kP * D / 16, 4>();
+            if (first) raise(sc[1], 2, t0, part);
+            read_group(v_lds + cur + 32 * S::kVRow, 0);
+            score(sc[0], 0, pg[1]);
+            weigh(sc[1], 0, w8[1], sum, rsum, true);
+            stay(sc[0]);
+            interleave<NB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
+            settle(sc[1], 2, t0, w8[1]);
+            __syncthreads();  // the next tile's values are there, those before this one's are done with
+            before = cur;
+            cur = next;
+  #pragma unroll
+            for (int u = 0; u < kRuns; ++u) pg[0][u] = pg[1][u], pg[1][u] = pg[2][u];
           }
-#pragma unroll
-          for (int b = 0; b < MB; ++b) l_run[b] += sum[b], r_run[b] += rsum[b];
-        };
-        score(sc[0], 0, pg[0]);
-        __syncthreads();
-        read_group(v_lds + 32 * S::kVRow, 0);  // multiplied with weights of zero
-        for (int s = s0; s < s1; ++s) {
-          const int t0 = (s * WT + wt) * S::kTile;
-          const bool part = t0 + S::kTile > all_seen;
-          const int next = cur == 2 * kSlot ? 0 : cur + kSlot;
-          pages_of(s + 2, entry, pg[2]);
-          look_up(s + 3, entry);
-          const bool first = part || s == s0;
-          // Two workgroups share a compute unit, and the older one's waves always go
-          // first: it ended at 580 us where the other needed 740.  They take turns at a
-          // higher priority instead, 41 us each by the device's clock (prompts of 8000 rows: 690 us, in turn 650).
-          if ((uint32_t)__builtin_readsteadycounter() >> 12 & 1 ^ (blockIdx.x >= gridDim.x / 2)) __builtin_amdgcn_s_setprio(1);
-          else __builtin_amdgcn_s_setprio(0);
-          // What is loaded past the last tile lies in some page and is of no use; a
-          // branch around it would keep the products from running beside the rest.
-          // second half of the tile before, first half's weights, second half's scores
-          load_keys(s + 1, pg[1], 0);
-#pragma unroll
+  #pragma unroll
           for (int g = 0; g < kGroups; ++g) {
             if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
             add_group(g, w8[1]);
           }
-          interleave<MB * S::kP * D / 16, 2>();
-          if (first) raise(sc[0], 0, t0, part);
-          read_group(v_lds + cur, 0);
-          score(sc[1], 2, pg[0]);
-          weigh(sc[0], 0, w8[0], sum, rsum, true);
-          stay(sc[1]);
-          interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
-          settle(sc[0], 0, t0, w8[0]);
-          // first half of this tile, second half's weights, the next tile's scores
-          load_keys(s + 1, pg[1], 2);
-#pragma unroll
-          for (int g = 0; g < kGroups; ++g) {
-            if (g + 1 < kGroups) read_group(v_lds + cur, g + 1);
-            add_group(g, w8[0]);
-          }
-#pragma unroll
-          for (int j = 0; j < kVMine; ++j) unpack(j, pg[1], v_lds + next, 0);
-          load_values(s + 2, pg[2]);
-          interleave<MB * S::kP * D / 16, 4>();
-          if (first) raise(sc[1], 2, t0, part);
-          read_group(v_lds + cur + 32 * S::kVRow, 0);
-          score(sc[0], 0, pg[1]);
-          weigh(sc[1], 0, w8[1], sum, rsum, true);
-          stay(sc[0]);
-          interleave<MB * 2 * AttnQuery<S>::kProducts * S::kKSteps, 8>();
-          settle(sc[1], 2, t0, w8[1]);
-          __syncthreads();  // the next tile's values are there, those before this one's are done with
-          before = cur;
-          cur = next;
-#pragma unroll
-          for (int u = 0; u < kRuns; ++u) pg[0][u] = pg[1][u], pg[1][u] = pg[2][u];
-        }
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          if (g + 1 < kGroups) read_group(v_lds + before + 32 * S::kVRow, g + 1);
-          add_group(g, w8[1]);
-        }
+        };
+        if (MB > 1 && m0 + (WM + wm) * 16 >= rows_m) run(Blocks<1>{});
+        else run(Blocks<MB>{});
       }
     }
 
@@ -852,7 +866,7 @@ void kv_attention_kernel(KvAttnParams p) {
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
         const float l = cross_row_sum(l_run[b]), r = S::kP == 1 ? cross_row_sum(r_run[b]) : l;
-        const int m_in = (wm * MB + b) * 16 + col;
+        const int m_in = (b * WM + wm) * 16 + col;
         if (row_i[b] < 0) continue;
         if (whole) {
           const int64_t row = ((int64_t)q * p.cap + row_i[b]) * p.q_heads + head * g_rows + (m0 + m_in - row_i[b] * g_rows);
@@ -875,16 +889,16 @@ void kv_attention_kernel(KvAttnParams p) {
         l_run[b] = cross_row_sum(l_run[b]);
         r_run[b] = S::kP == 1 ? cross_row_sum(r_run[b]) : l_run[b];
         if (quarter == 0) {
-          m_lds[wt][(wm * MB + b) * 16 + col] = m_run[b];
-          l_lds[wt][(wm * MB + b) * 16 + col] = l_run[b];
-          r_lds[wt][(wm * MB + b) * 16 + col] = r_run[b];
+          m_lds[wt][(b * WM + wm) * 16 + col] = m_run[b];
+          l_lds[wt][(b * WM + wm) * 16 + col] = l_run[b];
+          r_lds[wt][(b * WM + wm) * 16 + col] = r_run[b];
         }
       }
       __syncthreads();
       float* o_lds = reinterpret_cast<float*>(lds);
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
-        const int mine_row = (wm * MB + b) * 16 + col;
+        const int mine_row = (b * WM + wm) * 16 + col;
         float top = kNegInf;
 #pragma unroll
         for (int u = 0; u < WT; ++u) top = fmaxf(top, m_lds[u][mine_row]);
@@ -895,7 +909,7 @@ void kv_attention_kernel(KvAttnParams p) {
         __syncthreads();
         for (int x = tid; x < WM * 16 * (D / 8); x += S::kThreads) {
           const int row = x / (D / 8), d = x % (D / 8) * 8;  // row: of the waves' blocks b
-          const int m_in = ((row / 16) * MB + b) * 16 + row % 16, m = m0 + m_in;
+          const int m_in = (b * WM + row / 16) * 16 + row % 16, m = m0 + m_in;
           if (m >= rows_m) continue;
           float top2 = kNegInf;
 #pragma unroll
