@@ -77,10 +77,13 @@ struct AttnPlan {
 // The tile: the smallest that holds all rows of a request and kv head, so that its
 // keys and values are read once, up to the largest, whose waves share them (64
 // trees of up to 65 rows and 4 query heads a kv head over 500 to 8000 tokens: tiles
-// of 128 rows 192 us, of 32 257, of 16 304).  A few tiles cut into many pieces
+// of 128 rows 188 us, of 32 257, of 16 304; of 12 rows: 89 us, 119 in tiles of 32; of
+// 7 rows: 80 either way, 90 in tiles of 16).  A few tiles cut into many pieces
 // cost more in partial results than they gain, unless their context is long: one
 // such tree over 5003 tokens took 40 us in tiles of 128 and 34 in tiles of 32,
 // three of 33 rows in fp32 over 50 to 700 27 us in tiles of 64 and 21 in tiles of 16.
+// Up to 64 rows that holds for long contexts too (one tree of 12 rows over 30000
+// tokens: tiles of 32 29 us, of 128 36; four of 9 rows over 20000: 48 and 45).
 //
 // The workgroups: what a compute unit holds of them, so that none waits.  Tiles of
 // 16 rows would allow three; few of them are cut into two thirds as many pieces
@@ -88,11 +91,12 @@ struct AttnPlan {
 AttnPlan attn_plan(const ts_kv_cache* c, int32_t R, int32_t cap, int32_t q_heads, int32_t dtype, int64_t tokens, int cus) {
   AttnPlan x;
   const int64_t rows = (int64_t)cap * (q_heads / c->heads), most = dtype == TS_F32 ? 64 : 128;
-  const bool few = (int64_t)R * c->heads * ((rows + most - 1) / most) * 4 < cus, brief = few && tokens > 0 && tokens <= 16384;
+  const int64_t pairs = (int64_t)R * c->heads;  // of requests and kv heads
+  const bool few = pairs * ((rows + most - 1) / most) * 4 < cus, brief = few && tokens > 0 && tokens <= 16384;
   if (dtype == TS_F32)
     x.tile = rows <= 16 || brief ? AttnTile::k16 : AttnTile::k64;
   else
-    x.tile = rows <= 16 ? AttnTile::k16 : rows <= 64 || brief ? AttnTile::k32 : AttnTile::k128;
+    x.tile = rows <= 16 ? AttnTile::k16 : rows <= 32 || brief || (rows <= 64 && pairs * 12 < cus) ? AttnTile::k32 : AttnTile::k128;
   x.rows = 16 << (int)x.tile;
   const bool small = x.tile == AttnTile::k16 || x.tile == AttnTile::k32;
   x.groups = cus * (c->head_dim == 256 ? 1 : x.tile == AttnTile::k16 && dtype == TS_BF16 && !few ? 3 : 2);
