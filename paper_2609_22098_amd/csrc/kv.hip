@@ -86,20 +86,21 @@ struct AttnPlan {
 // tokens: tiles of 32 29 us, of 128 36; four of 9 rows over 20000: 48 and 45).
 //
 // The workgroups: what a compute unit holds of them, so that none waits.  Tiles of
-// 16 rows would allow three; few of them are cut into two thirds as many pieces
-// (131001 tokens, 8 tiles: 40 us with two, 44 with three; 1024 tiles 125 and 122).
+// 16 rows would allow three, which is better where a unit has a tile or more (1024
+// tiles over 300 to 16000 tokens: 128 us with two, 124 with three; 256: 42.5 and 41.8;
+// 128 over 16000: 67 and 72; 8 over 131001: 38 and 41).
 AttnPlan attn_plan(const ts_kv_cache* c, int32_t R, int32_t cap, int32_t q_heads, int32_t dtype, int64_t tokens, int cus) {
   AttnPlan x;
   const int64_t rows = (int64_t)cap * (q_heads / c->heads), most = dtype == TS_F32 ? 64 : 128;
   const int64_t pairs = (int64_t)R * c->heads;  // of requests and kv heads
-  const bool few = pairs * ((rows + most - 1) / most) * 4 < cus, brief = few && tokens > 0 && tokens <= 16384;
+  const bool brief = tokens > 0 && tokens <= 16384 && pairs * ((rows + most - 1) / most) * 4 < cus;
   if (dtype == TS_F32)
     x.tile = rows <= 16 || brief ? AttnTile::k16 : AttnTile::k64;
   else
     x.tile = rows <= 16 ? AttnTile::k16 : rows <= 32 || brief || (rows <= 64 && pairs * 12 < cus) ? AttnTile::k32 : AttnTile::k128;
   x.rows = 16 << (int)x.tile;
   const bool small = x.tile == AttnTile::k16 || x.tile == AttnTile::k32;
-  x.groups = cus * (c->head_dim == 256 ? 1 : x.tile == AttnTile::k16 && dtype == TS_BF16 && !few ? 3 : 2);
+  x.groups = cus * (c->head_dim == 256 ? 1 : x.tile == AttnTile::k16 && dtype == TS_BF16 && pairs >= cus ? 3 : 2);
   x.min_tokens = small ? 256 : 64;  // a step
   // Four steps of small tiles, six of tiles of 32 that have a compute unit each,
   // sixteen of large ones that fill the device, take less than cutting and joining:
