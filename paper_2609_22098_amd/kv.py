@@ -70,10 +70,11 @@ _I32 = torch.int32
 
 
 def _int32(name, t, shape, device):
-    """The address of a contiguous int32 tensor of that shape on that GPU."""
-    if t.dtype is _I32 and t.shape == shape and t.get_device() == device and t.is_contiguous():
+    """The address of a contiguous int32 tensor of that shape on that GPU (host tensors are on device -1)."""
+    if t.dtype is _I32 and t.shape == shape and t.get_device() == device >= 0 and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{name}: a contiguous int32 tensor {list(shape)} on cuda:{device} is needed, got {t.dtype} "
+    where = f"cuda:{device}" if device >= 0 else "a GPU"
+    raise ValueError(f"{name}: a contiguous int32 tensor {list(shape)} on {where} is needed, got {t.dtype} "
                      f"{list(t.shape)} on {t.device}")
 
 

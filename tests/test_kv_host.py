@@ -1,0 +1,49 @@
+"""The cache's binding on the host: what must never reach the library (which a stub stands in for)."""
+import pytest
+
+from paper_2609_22098_amd import kv
+
+torch = pytest.importorskip("torch")
+
+
+class _Library:
+    """Stands in for the library and counts the calls that reach it."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def entry(*args):
+            self.calls.append((name, args))
+            return 0
+        return entry
+
+
+@pytest.fixture
+def library(monkeypatch):
+    stub = _Library()
+    monkeypatch.setattr(kv, "lib", lambda: stub)
+    monkeypatch.setattr(kv, "_current_stream", lambda device: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    return stub
+
+
+def _given(R=2, pages=6, blocks=4):
+    i32 = dict(dtype=torch.int32)
+    return dict(free_pages=torch.arange(pages, **i32), free_count=torch.full((1,), pages, **i32),
+                held=torch.zeros((R,), **i32), table=torch.full((R, blocks), -1, **i32))
+
+
+def test_a_pool_on_the_host_is_refused(library):
+    """Host tensors agree among themselves about their device; a pool of them never gets as far as a plan."""
+    length = n = torch.zeros((2,), dtype=torch.int32)
+    for make in (lambda: kv.Pool(6, 2, 4, 16, device="cpu"), lambda: kv.Pool(6, 2, 4, 16, **_given())):
+        with pytest.raises(ValueError):
+            kv.plan(make(), length, n, 3)
+    assert not library.calls
+
+
+def test_no_address_is_taken_of_a_host_tensor(library):
+    """Not even where a device of -1, which host tensors report, is asked for."""
+    with pytest.raises(ValueError):
+        kv._int32("n", torch.zeros((2,), dtype=torch.int32), (2,), -1)
