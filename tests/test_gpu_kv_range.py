@@ -1,0 +1,78 @@
+"""The cache attention at the ends of what its header allows: scores whose products the matrix unit cuts off most,
+numbers near the ends of their types.  Oracles are plain numpy in 64 bits."""
+import numpy as np
+import pytest
+
+import kv_ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2609_22098_amd import kv
+    kv.lib()
+    return t
+
+
+def _dev(torch, a, dtype=np.int32):
+    return torch.from_numpy(np.ascontiguousarray(a).astype(dtype)).cuda()
+
+
+def _one_token(torch, q, k, scale, dtype):
+    """Query heads q [R][hq][D] on one token each, keys k [R][heads][D] (values of the format): the log-sum-exp, which is
+    the score, and the output over values of ones."""
+    from paper_2609_22098_amd import kv
+    R, hq, D = q.shape
+    heads = k.shape[1]
+    ref = kv_ref.Cache(R, 16, heads, D)
+    ref.k[::16], ref.v[:] = k, 1.0
+    cache = kv.Cache(torch.from_numpy(kv_ref.pack(ref, 1).copy()).cuda(), 16, heads, D)
+    q = torch.from_numpy(q[:, None]).to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+    lse = torch.full((R, 1, hq), 99.0, device="cuda")
+    zero = _dev(torch, np.zeros(R))
+    out, _ = kv.attention(cache, q, zero, zero, _dev(torch, np.arange(R)[:, None]), scale=scale, lse=lse)
+    return lse.double().cpu().numpy()[:, 0], out.double().cpu().numpy()[:, 0]
+
+
+# ---------------------------------------------------------------- products that are cut off
+
+
+# (query, key) of the largest of eight neighbouring elements, and of the seven others: a query that rounds up to the next
+# power of two where it is held in 4 bits, beside the least that those bits show; a product 2^13 above its neighbours;
+# queries that leave as much as one can to their second part, beside products just too small for that; and two that
+# round up beside such.
+DOMINATED = [((3.90625, 6.0), (2.0 ** -9, 0.5)), ((3.5, 6.0), (2.0 ** -9, 1.0)), ((2.125, 4.0), (1.875 * 2.0 ** -15, 1.0)),
+             ((3.125, 4.0), (1.875 * 2.0 ** -15, 1.0)), ((1.9375, 6.0), (1.875 * 2.0 ** -10, 0.5)),
+             ((3.96875, 4.0), (1.75 * 2.0 ** -14, 1.5))]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("case", range(len(DOMINATED)))
+def test_scores_with_one_large_product_in_eight(torch, case, D):
+    """One channel of queries and keys far above its neighbours, in one group of eight or in all.  Off by at most what
+    the header states: of eight products the matrix unit cuts off what lies below 2^-13 of the largest's power of
+    two.  The first part of a query loses nothing of that; the second, at most 2^-4 of an element, less than 7 * 2^-17 of
+    the largest |Q| |K| of the eight; 64 sums in 32 bits add 64 * 2^-24 of all."""
+    (q0, k0), (q1, k1) = DOMINATED[case]
+    rng = np.random.default_rng(case)
+    R, heads, group = 32, 2, 2
+    at = rng.integers(0, 8, (R, heads, D // 8, 1))  # the large one's place among its eight
+    large = np.arange(8) == at
+    some = rng.random((R, heads, D // 8, 1)) < np.where(np.arange(R) % 2, 1.0, 0.1)[:, None, None, None]
+    some[:, :, 0] = True
+    k = np.where(large & some, k0, k1).reshape(R, heads, D)
+    q = np.where(large & some, q0, q1).reshape(R, heads, 1, D) * np.array([1.0, -0.125])[:, None]
+    sign = np.where(rng.random((R, heads, D)) < np.where(np.arange(R) % 4 < 2, 0.0, 0.5)[:, None, None], -1.0, 1.0)
+    k, q = k * sign, q * sign[:, :, None]  # products of one sign: what is cut off adds up
+    q = q * 2.0 ** rng.integers(-20, 20, (R, 1, 1, 1))
+    scale = 0.25
+    got, _ = _one_token(torch, q.reshape(R, heads * group, D), k, scale, "bf16")
+    want = scale * (q * k[:, :, None]).sum(-1).reshape(R, -1)
+    mag = np.abs(q * k[:, :, None]).sum(-1).reshape(R, -1)
+    held = (np.abs(q).max(-1) * np.abs(k[:, :, None]).sum(-1)).reshape(R, -1)
+    bound = scale * (2.0 ** -14 * mag + 2.0 ** -18 * held) + 2.0 ** -22 * np.abs(want)
+    over = np.abs(got - want) / bound
+    assert over.max() <= 1, (over.max(), np.unravel_index(over.argmax(), over.shape))
