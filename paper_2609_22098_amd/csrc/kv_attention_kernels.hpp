@@ -87,6 +87,7 @@ struct AttnQuery;
 template <typename S>
 struct AttnQuery<S, false> {
   i32x8 w[S::kKSteps][2];
+  int scales;  // of the pieces, a byte each: products come out as <Q, K> itself, whatever the query's size
 
   // The lane's elements as they are, and a step that uses them apart from it, so
   // that other loads can be sent in between.
@@ -102,8 +103,7 @@ struct AttnQuery<S, false> {
       }
   }
 
-  // Returns what a product's score is multiplied by to give base-2 units.
-  __device__ __forceinline__ float convert(float scale_log2) {
+  __device__ __forceinline__ void convert(bool negative) {
     float v[S::kKSteps][32];
     uint32_t top = 0;
 #pragma unroll
@@ -119,10 +119,12 @@ struct AttnQuery<S, false> {
         }
     top = max(top, (uint32_t)xor16_i32((int)top));
     top = max(top, (uint32_t)xor32_i32((int)top));
-    // x * 2^(128 - e) has its largest in [1.9375, 3.875), which E4M3 rounds to at most 3.75
-    const int e = max((int)((top + 0x80000u) >> 23), 2);
+    // x * 2^(128 - e) has its largest in [1.9375, 3.875), which E4M3 rounds to at most 3.75 (below
+    // 2^-118 it stays smaller, so that both scales are bytes: bf16's least is a whole step there)
+    const int e = max((int)((top + 0x80000u) >> 23), 9);
+    scales = (e - 1) | (e - 9) << 8;
     const bool finite = top < 0x7F800000u;  // else up is 0, and not-a-number comes of it
-    const float up = (scale_log2 < 0.f ? -1.f : 1.f) *
+    const float up = (negative ? -1.f : 1.f) *
                      __uint_as_float(e < 255 ? (uint32_t)(255 - e) << 23 : finite ? 0x400000u : 0u);
 #pragma unroll
     for (int k = 0; k < S::kKSteps; ++k)
@@ -141,16 +143,14 @@ struct AttnQuery<S, false> {
         word = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         w[k][1][u] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], word, true);
       }
-    // never 0, so that a hidden score's -inf stays one
-    return fmaxf(__builtin_fabsf(scale_log2) * __uint_as_float((uint32_t)max(e - 1, 1) << 23), 1e-36f);
   }
 
   // Product `i` of kProducts with 128 elements of 16 keys: small ones first.
   static constexpr int kProducts = 2;
   __device__ __forceinline__ f32x4 product(int i, i32x4 codes, int scale, int k, f32x4 acc) const {
     const i32x8 a = {codes[0], codes[1], codes[2], codes[3], 0, 0, 0, 0};
-    return i == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][1], acc, 4, 0, 0, scale, 0, 127 - 8)
-                  : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][0], acc, 4, 0, 0, scale, 0, 127);
+    return i == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][1], acc, 4, 0, 0, scale, 1, scales)
+                  : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w[k][0], acc, 4, 0, 0, scale, 0, scales);
   }
 };
 
@@ -167,20 +167,19 @@ struct AttnQuery<S, true> {
         raw[k][u] = *reinterpret_cast<const f32x4*>(x + k * 128 + (S::D < 128 ? quarter & 1 : quarter) * 32 + u * 4);
   }
 
-  __device__ __forceinline__ float convert(float scale_log2) {
+  __device__ __forceinline__ void convert(bool negative) {
 #pragma unroll
     for (int k = 0; k < S::kKSteps; ++k)
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
         const float y = raw[k][j / 4][j % 4];
-        float left = scale_log2 < 0.f ? -y : y;
+        float left = negative ? -y : y;
 #pragma unroll
         for (int piece = 0; piece < 3; ++piece) {
           w[k][j / 8][piece][j % 8] = (__bf16)left;
           left -= (float)w[k][j / 8][piece][j % 8];
         }
       }
-    return fmaxf(__builtin_fabsf(scale_log2), 1e-36f);
   }
 
   static constexpr int kProducts = 12;
@@ -522,7 +521,9 @@ void kv_attention_kernel(KvAttnParams p) {
     look_up(s0, entry);
     // queries: those of rows past the last read row 0 and are of no use
     AttnQuery<S> qp[MB];
-    float c_row[MB];
+    // what <Q, K>, queries with the scale's sign, is multiplied by to give base-2 units; never
+    // 0, so that a hidden score's -inf stays one
+    const float unit = fmaxf(__builtin_fabsf(p.scale_log2), 1e-36f);
     int row_i[MB];
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
@@ -542,7 +543,7 @@ void kv_attention_kernel(KvAttnParams p) {
     look_up(s0 + 1 + kAhead, entry);
 
 #pragma unroll
-    for (int b = 0; b < MB; ++b) c_row[b] = qp[b].convert(p.scale_log2);
+    for (int b = 0; b < MB; ++b) qp[b].convert(p.scale_log2 < 0.f);
 
     char* v_lds = lds + wt * (S::kVTokens * S::kVRow);
     constexpr int kGroups = D / 64;  // of four blocks of 16 elements
@@ -608,7 +609,7 @@ void kv_attention_kernel(KvAttnParams p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) top[b] = fmaxf(top[b], x[b][u][e]);
         top[b] = fmaxf(top[b], xor16_f32(top[b]));
-        top[b] = fmaxf(top[b], xor32_f32(top[b])) * c_row[b];
+        top[b] = fmaxf(top[b], xor32_f32(top[b])) * unit;
       }
     };
     // Raises what weights are taken against to the maximum `top`, which it may lag
@@ -635,7 +636,7 @@ void kv_attention_kernel(KvAttnParams p) {
     // for the log-sum-exp, and as the products take them, which is what outputs are
     // divided by, so that the rounding of a row's large weights cancels.
     // `fused`: with one rounding instead of two.  The maximum was rounded when it was
-    // taken times c_row: a weight against it is then off by a factor of up to
+    // taken times `unit`: a weight against it is then off by a factor of up to
     // 2^(|m| 2^-24), the same for all of a row, which must not be large.
     auto weigh = [&](const auto& x, int u0, auto& w8, auto& sum, auto& rsum, bool fused) {
       constexpr int NB = sizeof(x) / sizeof(x[0]);
@@ -645,8 +646,8 @@ void kv_attention_kernel(KvAttnParams p) {
         rsum[b] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float left = exp2_fast(fused ? __builtin_fmaf(x[b][u0 + e / 4][e % 4], c_row[b], m_neg[b])
-                                       : x[b][u0 + e / 4][e % 4] * c_row[b] + m_neg[b]);
+          float left = exp2_fast(fused ? __builtin_fmaf(x[b][u0 + e / 4][e % 4], unit, m_neg[b])
+                                       : x[b][u0 + e / 4][e % 4] * unit + m_neg[b]);
           sum[b] += left;
 #pragma unroll
           for (int piece = 0; piece < S::kP; ++piece) {

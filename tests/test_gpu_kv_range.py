@@ -76,3 +76,67 @@ def test_scores_with_one_large_product_in_eight(torch, case, D):
     bound = scale * (2.0 ** -14 * mag + 2.0 ** -18 * held) + 2.0 ** -22 * np.abs(want)
     over = np.abs(got - want) / bound
     assert over.max() <= 1, (over.max(), np.unravel_index(over.argmax(), over.shape))
+
+
+# ---------------------------------------------------------------- the ends of the types
+
+
+# Exponents of queries, keys and the scale: a scale times a query, and a query scaled to one times a key, that pass fp32
+# where the score does not; queries and keys next to the largest and the least of their types.
+FAR = [(30, -123, 100), (-100, 122, -18), (127, -123, 0), (-118, 122, 0), (-126, 100, 30), (60, -20, -36), (-60, -20, 84),
+       (100, -110, 20), (-133, 122, 15), (-126, 122, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 256])
+@pytest.mark.parametrize("case", range(len(FAR)))
+def test_scores_of_far_exponents(torch, case, D, dtype):
+    """Scores of ordinary size from queries, keys and scales that are far from it; <Q, K> itself is an fp32 number.  The
+    bounds are the header's, and in fp32 D + 8 roundings of the sum of magnitudes."""
+    eq, ek, es = FAR[case]
+    rng = np.random.default_rng(case)
+    R, heads, group = 16, 2, 3
+    q = rng.integers(-127, 128, (R, heads, group, D)) / 64.0
+    q[..., 3] = 127 / 64  # the largest, in bf16 too; whole steps of the least subnormal at 2^-133 are few
+    q = np.rint(q) if eq < -126 else q
+    k = kv_ref.rounded(rng.standard_normal((R, heads, D)) * 2.0 ** (ek - 1), np.ones((R, heads, D)))[0]
+    same = (np.arange(R) % 2 == 0)[:, None, None, None]  # half of the rows: products of one sign
+    q, scale = np.where(same, np.abs(q) * np.sign(k)[:, :, None], q) * 2.0 ** eq, 2.0 ** es * -0.75
+    got, out = _one_token(torch, q.reshape(R, heads * group, D), k, scale, dtype)
+    want = scale * (q * k[:, :, None]).sum(-1).reshape(R, -1)
+    mag = np.abs(q * k[:, :, None]).sum(-1).reshape(R, -1)
+    held = (np.abs(q).max(-1) * np.abs(k[:, :, None]).sum(-1)).reshape(R, -1)
+    bound = 2.0 ** -14 * mag + 2.0 ** -18 * held if dtype == "bf16" else (D + 8) * 2.0 ** -24 * mag
+    over = np.abs(got - want) / (abs(scale) * bound + 2.0 ** -22 * np.abs(want))
+    assert over.max() <= 1, (over.max(), np.unravel_index(over.argmax(), over.shape))
+    assert (out == 1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 30, 70])
+def test_queries_that_are_not_finite(torch, rows, dtype):
+    """A query with an infinity or a not-a-number gives not-a-number, and no other row is touched by it."""
+    from paper_2609_22098_amd import kv
+    rng = np.random.default_rng(rows)
+    heads, hq, D, context = 2, 6, 128, 90
+    ref = kv_ref.Cache(-(-(context + rows) // 16), 16, heads, D)
+    ref.k, ref.v = kv_ref.rounded(rng.standard_normal(ref.k.shape), rng.standard_normal(ref.v.shape))
+    cache = kv.Cache(torch.from_numpy(kv_ref.pack(ref, 1).copy()).cuda(), 16, heads, D)
+    table = _dev(torch, np.arange(len(ref.k) // 16)[None])
+    q = torch.from_numpy(rng.standard_normal((1, rows, hq, D))).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    args = _dev(torch, [context]), _dev(torch, [rows - 1]), table
+
+    def run(x):
+        lse = torch.full((1, rows, hq), 99.0, device="cuda")
+        out, _ = kv.attention(cache, x.cuda(), *args, lse=lse)
+        return out, lse
+
+    want, wl = run(q)
+    bad = torch.zeros((1, rows, hq), dtype=torch.bool)
+    for i, (at, x) in enumerate(((5, float("inf")), (127, -float("inf")), (64, float("nan")))):
+        q[0, rows // 2, 2 * i, at] = x
+        bad[0, rows // 2, 2 * i] = True
+    out, lse = run(q)
+    bad = bad.cuda()
+    assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all()
+    assert torch.equal(out[~bad], want[~bad]) and torch.equal(lse[~bad], wl[~bad])
