@@ -103,7 +103,8 @@ struct AttnQuery<S, false> {
       }
   }
 
-  __device__ __forceinline__ void convert(bool negative) {
+  // sign: the scale's, 0 for none.
+  __device__ __forceinline__ void convert(float sign) {
     float v[S::kKSteps][32];
     uint32_t top = 0;
 #pragma unroll
@@ -124,8 +125,7 @@ struct AttnQuery<S, false> {
     const int e = max((int)((top + 0x80000u) >> 23), 9);
     scales = (e - 1) | (e - 9) << 8;
     const bool finite = top < 0x7F800000u;  // else up is 0, and not-a-number comes of it
-    const float up = (negative ? -1.f : 1.f) *
-                     __uint_as_float(e < 255 ? (uint32_t)(255 - e) << 23 : finite ? 0x400000u : 0u);
+    const float up = sign * __uint_as_float(e < 255 ? (uint32_t)(255 - e) << 23 : finite ? 0x400000u : 0u);
 #pragma unroll
     for (int k = 0; k < S::kKSteps; ++k)
 #pragma unroll
@@ -167,13 +167,13 @@ struct AttnQuery<S, true> {
         raw[k][u] = *reinterpret_cast<const f32x4*>(x + k * 128 + (S::D < 128 ? quarter & 1 : quarter) * 32 + u * 4);
   }
 
-  __device__ __forceinline__ void convert(bool negative) {
+  __device__ __forceinline__ void convert(float sign) {
 #pragma unroll
     for (int k = 0; k < S::kKSteps; ++k)
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
         const float y = raw[k][j / 4][j % 4];
-        float left = negative ? -y : y;
+        float left = sign * y;
 #pragma unroll
         for (int piece = 0; piece < 3; ++piece) {
           w[k][j / 8][piece][j % 8] = (__bf16)left;
@@ -521,9 +521,10 @@ void kv_attention_kernel(KvAttnParams p) {
     look_up(s0, entry);
     // queries: those of rows past the last read row 0 and are of no use
     AttnQuery<S> qp[MB];
-    // what <Q, K>, queries with the scale's sign, is multiplied by to give base-2 units; never
-    // 0, so that a hidden score's -inf stays one
-    const float unit = fmaxf(__builtin_fabsf(p.scale_log2), 1e-36f);
+    // what <Q, K> is multiplied by to give base-2 units, queries with the scale's sign; a scale of
+    // 0 is one of 1 on queries of 0, so that a hidden score's -inf stays one
+    const float sign = p.scale_log2 == 0.f ? 0.f : p.scale_log2 < 0.f ? -1.f : 1.f;
+    const float unit = p.scale_log2 == 0.f ? 1.f : __builtin_fabsf(p.scale_log2);
     int row_i[MB];
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
@@ -543,7 +544,7 @@ void kv_attention_kernel(KvAttnParams p) {
     look_up(s0 + 1 + kAhead, entry);
 
 #pragma unroll
-    for (int b = 0; b < MB; ++b) qp[b].convert(p.scale_log2 < 0.f);
+    for (int b = 0; b < MB; ++b) qp[b].convert(sign);
 
     char* v_lds = lds + wt * (S::kVTokens * S::kVRow);
     constexpr int kGroups = D / 64;  // of four blocks of 16 elements

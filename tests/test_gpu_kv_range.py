@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 import kv_ref
+from test_gpu_kv import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -140,3 +141,14 @@ def test_queries_that_are_not_finite(torch, rows, dtype):
     bad = bad.cuda()
     assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all()
     assert torch.equal(out[~bad], want[~bad]) and torch.equal(lse[~bad], wl[~bad])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-37, -1e-37, 1e-45])
+@pytest.mark.parametrize("rows,reach", [(1, 0), (1, 17000), (40, 0), (70, 0), (70, 17000)])
+def test_scales_next_to_zero(torch, rows, reach, scale, dtype):
+    """Keys near 1e35 under a scale of zero weigh alike, under one of 1e-37 by their scores of about one; what the mask
+    hides has no weight under either."""
+    c = Case(torch, [100, 0], [rows - 1, max(rows - 3, 0)], rows, 4, 2, 128, 16, dtype, True, seed=rows, reach=reach, kscale=1e35)
+    c.scale = scale
+    c.check(torch)
