@@ -156,6 +156,7 @@ struct AttnQuery<S, false> {
 
 template <typename S>
 struct AttnQuery<S, true> {
+  static constexpr float kBf16Max = 0x1.FEp127f;
   bf16x8 w[S::kKSteps][4][3];
 
   f32x4 raw[S::kKSteps][8];
@@ -176,7 +177,8 @@ struct AttnQuery<S, true> {
         float left = sign * y;
 #pragma unroll
         for (int piece = 0; piece < 3; ++piece) {
-          w[k][j / 8][piece][j % 8] = (__bf16)left;
+          // bf16's largest number, where rounding would pass it; an infinity still leaves one
+          w[k][j / 8][piece][j % 8] = (__bf16)(piece ? left : fminf(fmaxf(left, -kBf16Max), kBf16Max));
           left -= (float)w[k][j / 8][piece][j % 8];
         }
       }

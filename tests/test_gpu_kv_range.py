@@ -152,3 +152,21 @@ def test_scales_next_to_zero(torch, rows, reach, scale, dtype):
     c = Case(torch, [100, 0], [rows - 1, max(rows - 3, 0)], rows, 4, 2, 128, 16, dtype, True, seed=rows, reach=reach, kscale=1e35)
     c.scale = scale
     c.check(torch)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_largest_fp32_queries(torch, D):
+    """fp32 queries up to the type's largest number, which bf16, a part of them, would round to infinity."""
+    rng = np.random.default_rng(D)
+    R, heads, group = 8, 2, 3
+    top = float(np.finfo(np.float32).max)
+    q = rng.choice([top, -top, 3.4e38, 3.397e38, -3.3961775e38, 1.0, -3e38], (R, heads, group, D))
+    q = q.astype(np.float32).astype(np.float64)
+    k = kv_ref.rounded(rng.standard_normal((R, heads, D)) * 2.0 ** -110, np.ones((R, heads, D)))[0]
+    scale = 2.0 ** -15
+    got, out = _one_token(torch, q.reshape(R, heads * group, D), k, scale, "f32")
+    want = scale * (q * k[:, :, None]).sum(-1).reshape(R, -1)
+    mag = scale * np.abs(q * k[:, :, None]).sum(-1).reshape(R, -1)
+    over = np.abs(got - want) / ((D + 8) * 2.0 ** -24 * mag + 2.0 ** -22 * np.abs(want))  # fp32 sums of D products
+    assert over.max() <= 1, (over.max(), np.unravel_index(over.argmax(), over.shape))
+    assert (out == 1).all()
