@@ -144,7 +144,8 @@ size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32
  *      (bits past row n[q] do not count), or NULL;
  *   scale: below 2^127 in magnitude (usually head_dim^-0.5).  <Q, K_t> is an fp32
  *      number and so is the score: what passes 2^128 is infinite (or, where sums
- *      of both signs pass it, not-a-number);
+ *      of both signs pass it, not-a-number).  A score of -inf has weight 0, and a row
+ *      of no other sees nothing; one of +inf makes its row not-a-number;
  *   out: DEVICE [R][cap][q_heads][head_dim] of dtype, 16-byte aligned; lse (may
  *      be NULL): DEVICE float [R][cap][q_heads], log sum_t exp(scale <Q, K_t>).
  *      Rows past n[q] of both are left as they were.  Neither may overlap an

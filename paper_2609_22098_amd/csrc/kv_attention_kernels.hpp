@@ -400,11 +400,15 @@ void kv_attention_kernel(KvAttnParams p) {
     const int32_t* table = p.table + (size_t)q * p.max_blocks;
 
     // ---- tokens
-    float m_run[MB], m_neg[MB], l_run[MB], r_run[MB];  // the maximum, its negative (0 for none), the sums of weights
+    // Where waves share values, weights are taken with one rounding against maxima up
+    // to kFused; a row that has seen no score above -inf yet counts as past that, so
+    // that it looks for one in every half tile.
+    constexpr float kFused = 4194304.f, kNone = WM > 1 ? 2.f * kFused : 0.f;  // 2^22
+    float m_run[MB], m_neg[MB], l_run[MB], r_run[MB];  // the maximum, its negative (kNone for none), the sums of weights
     f32x4 o[MB][D / 16];
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
-      m_run[b] = kNegInf, m_neg[b] = 0.f, l_run[b] = 0.f, r_run[b] = 0.f;
+      m_run[b] = kNegInf, m_neg[b] = kNone, l_run[b] = 0.f, r_run[b] = 0.f;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -534,6 +538,7 @@ void kv_attention_kernel(KvAttnParams p) {
       const bool there = m < rows_m;
       const int i = there ? m / g_rows : 0, g = there ? m - i * g_rows : 0;
       row_i[b] = there ? i : -1;
+      if (WM > 1 && !there) m_run[b] = 0.f, m_neg[b] = 0.f;
       qp[b].fetch(static_cast<const TE*>(p.q) + ((int64_t)q * p.cap + i) * p.q_stride + (int64_t)(head * g_rows + g) * D, quarter);
     }
     pages_of(s0, entry, pg[0]);
@@ -628,7 +633,7 @@ void kv_attention_kernel(KvAttnParams p) {
           const float m_new = fmaxf(m_run[b], top[b]);
           const float keep = m_new == kNegInf ? 1.f : exp2_fast(m_run[b] - m_new);
           m_run[b] = m_new;
-          m_neg[b] = m_new == kNegInf ? 0.f : -m_new;
+          m_neg[b] = m_new == kNegInf ? kNone : -m_new;
           l_run[b] *= keep;
           r_run[b] *= keep;
 #pragma unroll
@@ -778,7 +783,7 @@ void kv_attention_kernel(KvAttnParams p) {
   #pragma unroll
               for (int e = 0; e < 8; ++e) w8[1][b][piece][e] = (__bf16)0.f;
           float sum[NB], rsum[NB];
-          constexpr float kMost = 4096.f, kFused = 4194304.f;  // 2^22
+          constexpr float kMost = 4096.f;
           auto raise = [&](auto& x, int u0, int t0, bool part) {
             if (part) hide(x, u0, t0);
             float top[NB];

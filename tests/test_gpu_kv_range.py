@@ -170,3 +170,56 @@ def test_largest_fp32_queries(torch, D):
     over = np.abs(got - want) / ((D + 8) * 2.0 ** -24 * mag + 2.0 ** -22 * np.abs(want))  # fp32 sums of D products
     assert over.max() <= 1, (over.max(), np.unravel_index(over.argmax(), over.shape))
     assert (out == 1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,rows,reach", [(1, 1, 0), (1, 1, 17000), (1, 40, 17000), (90, 70, 0), (90, 70, 17000), (40, 300, 17000)])
+@pytest.mark.parametrize("far", [32, 64, 200, 500])
+def test_scores_of_minus_infinity(torch, far, R, rows, reach, dtype):
+    """The first tokens' scores pass fp32 and are -inf, which is a weight of zero; the others', however low, have all of
+    it, in one step of a workgroup or in many."""
+    c = Case(torch, [501] * R, [rows - 1] * R, rows, 4, 1, 64, 16, dtype, False, seed=far, reach=reach)
+    pos = np.arange(501 + rows)
+    slot = c.table[:, pos // 16] * 16 + pos % 16
+    c.q[:] = c.q.abs() + 0.5
+    key = np.where(pos < far, -(2.0 ** 33), -(2.0 ** -95) * (1 + pos % 3))
+    c.ref.k[slot] = key[:, None, None]
+    c.scale = 2.0 ** 100
+    out, lse = c.run(torch)
+    for q in (0, R - 1):
+        k, v = c.rows_of(q, 501 + rows)
+        see = kv_ref.sees(501, rows, 501 + rows)[:, far:]
+        want, wl, mass, mag = kv_ref.attention(c.q[q].double().numpy(), k[far:], v[far:], see, c.scale)
+        assert np.isfinite(wl).all() and wl.max() < -1000
+        got, gl = out[q].double().cpu().numpy(), lse[q].double().cpu().numpy()
+        # a key's elements are alike, so max |Q| sum |K| is sum |Q| |K| times the largest |Q| (of 1.4 million normal
+        # numbers: below 7.5 + 0.5) over their mean (above 0.5), under 16: a score is off by what the header states of
+        # these, in fp32 by 72 roundings
+        d = mag * (2.0 ** -14 + 2.0 ** -18 * 16 if dtype == "bf16" else 72 * 2.0 ** -24)
+        small = (501 + rows + 16) * 2.0 ** -24 + 2.0 ** -22
+        assert (np.abs(gl - wl) <= d + small + 2.0 ** -22 * np.abs(wl)).all()
+        half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+        weight = (half if dtype == "bf16" else 0) + small
+        assert (np.abs(got - want) <= half * np.abs(want) + (np.expm1(2 * d)[..., None] + weight) * mass + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,rows,reach", [(1, 1, 17000), (1, 40, 0), (90, 70, 0), (40, 300, 17000)])
+def test_scores_of_plus_infinity(torch, R, rows, reach, dtype):
+    """One token whose scores pass fp32 makes not-a-number of the rows that see it and of no other; where every score
+    of a row is -inf the row gives what one that sees nothing gives."""
+    c = Case(torch, [400] * R, [rows - 1] * R, rows, 4, 1, 64, 16, dtype, False, seed=rows, reach=reach)
+    c.q[:] = c.q.abs() + 0.5
+    c.scale = 2.0 ** 100
+    pos = np.arange(400 + rows)
+    slot = c.table[:, pos // 16] * 16 + pos % 16
+    c.ref.k[slot] = -(2.0 ** -95)
+    c.ref.k[slot[0, 400 + rows // 2]] = 2.0 ** 33
+    c.ref.k[slot[R - 1, : 400 + rows // 2]] = -(2.0 ** 33) if R > 1 else -(2.0 ** -95)
+    out, lse = c.run(torch)
+    sees = torch.arange(rows, device="cuda") >= rows // 2
+    assert torch.isnan(out[0, sees]).all() and torch.isnan(lse[0, sees]).all()
+    assert out[0, ~sees].isfinite().all() and lse[0, ~sees].isfinite().all() and out[1 : R - 1].isfinite().all()
+    if R > 1:
+        assert (out[R - 1, ~sees] == 0).all() and torch.isneginf(lse[R - 1, ~sees]).all()
+        assert out[R - 1, sees].isfinite().all() and lse[R - 1, sees].isfinite().all()
