@@ -190,7 +190,8 @@ class Pool:
 
 def plan(pool: Pool, length, n, cap, slots=True, out=None, stream=None):
     """ts_kv_plan: pages for the rows 0..n[q] behind length[q] tokens of every request.  Returns (slot [R][cap],
-    granted [R]), int32; slot is None with slots=False (only the pages).  out = (slot, granted) reuses tensors."""
+    granted [R]), int32; slot is None with slots=False (only the pages).  out = (slot, granted) reuses tensors, a slot of
+    None there as with slots=False."""
     if stream is not None:
         with _on(stream, pool.device):
             return plan(pool, length, n, cap, slots, out)
@@ -200,7 +201,7 @@ def plan(pool: Pool, length, n, cap, slots=True, out=None, stream=None):
         slot = n.new_empty((R, cap)) if slots else None
         granted = n.new_empty((R,))
     else:
-        slot, granted = out
+        slot, granted = out if slots else (None, out[1])
         _int32("granted", granted, (R,), d)
         if slot is not None:
             _int32("slot", slot, (R, cap), d)

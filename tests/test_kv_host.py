@@ -47,3 +47,23 @@ def test_no_address_is_taken_of_a_host_tensor(library):
     """Not even where a device of -1, which host tensors report, is asked for."""
     with pytest.raises(ValueError):
         kv._int32("n", torch.zeros((2,), dtype=torch.int32), (2,), -1)
+
+
+def _pool(monkeypatch):
+    """A pool whose tensors pass for GPU tensors."""
+    monkeypatch.setattr(kv, "_int32", lambda name, t, shape, device: f"{name} {list(t.shape)}")
+    return kv.Pool(6, 2, 4, 16, **_given())
+
+
+def test_a_plan_without_slots_writes_none(library, monkeypatch):
+    """slots=False asks for pages alone, also where tensors are given; a slot of None among those says the same."""
+    pool = _pool(monkeypatch)
+    length = n = torch.zeros((2,), dtype=torch.int32)
+    slot, granted = torch.zeros((2, 3), dtype=torch.int32), torch.zeros((2,), dtype=torch.int32)
+    for slots, out, want in ((False, (slot, granted), None), (False, (None, granted), None), (True, (None, granted), None),
+                             (True, (slot, granted), slot), (False, None, None)):
+        got = kv.plan(pool, length, n, 3, slots=slots, out=out)
+        assert got[0] is want and (out is None or got[1] is granted)
+        name, args = library.calls[-1]
+        assert name == "ts_kv_plan" and args[11] == (None if want is None else slot.data_ptr())
+    assert kv.plan(pool, length, n, 3)[0].shape == (2, 3) and library.calls[-1][1][11]
