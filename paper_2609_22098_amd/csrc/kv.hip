@@ -223,7 +223,7 @@ int32_t ts_kv_read(const ts_kv_cache* cache, int32_t layer, int32_t layers, cons
 size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32_t cap, int32_t q_heads, int32_t dtype) {
   clear_error();
   if (check_cache(cache) || check_dtype(dtype) || R < 0 || R > kMaxRequests || cap < 1 || cap > TS_KV_MAX_CAP || q_heads < 1 ||
-      q_heads % cache->heads || q_heads / cache->heads > kMaxGroup)
+      q_heads % cache->heads || q_heads / cache->heads > kMaxGroup || (int64_t)R * cap * q_heads >= (int64_t)1 << 31)
     return 0;
   return attn_plan(cache, R, cap, q_heads, dtype, 0, compute_units()).bytes;
 }

@@ -67,3 +67,16 @@ def test_a_plan_without_slots_writes_none(library, monkeypatch):
         name, args = library.calls[-1]
         assert name == "ts_kv_plan" and args[11] == (None if want is None else slot.data_ptr())
     assert kv.plan(pool, length, n, 3)[0].shape == (2, 3) and library.calls[-1][1][11]
+
+
+def test_no_workspace_for_sizes_that_a_call_refuses():
+    """R * cap * q_heads of 2^31 and more; one row less has a size."""
+    import ctypes
+    from paper_2609_22098_amd import binding as b
+    c = kv.CacheStruct(0x1000, 1 << 20, 8704 * 2, 2, 10, 64, 2, 128)
+
+    def size(R, cap, hq):
+        return kv.lib().ts_kv_attention_workspace_size(ctypes.byref(c), R, cap, hq, b.TS_BF16)
+
+    assert size(65536, 1 << 13, 4) == 0 and size(65536, (1 << 13) - 1, 4) > 0
+    assert size(2048, 1 << 20, 2) == 0 and size(1023, 1 << 20, 2) > 0
