@@ -280,7 +280,7 @@ int32_t ts_kv_accept(const ts_kv_cache* cache, const int32_t* len, const int32_t
   TS_CHECK(check_requests(R, max_blocks, cache->page_size));
   if (R == 0) return TS_OK;
   if (!len || !n || !table || !path_nodes || !path_len || !new_len) return fail(TS_EINVAL, "a required array is NULL");
-  if (new_len == len || new_len == n || new_len == path_len)
+  if (new_len == len || new_len == n || new_len == table || new_len == path_nodes || new_len == path_len)
     return fail(TS_EINVAL, "new_len must not be one of the inputs");
   hipStream_t s = static_cast<hipStream_t>(stream);
   const KvAcceptParams p = {view(cache, 0), cache->layers, len, n, table, path_nodes, path_len, R, max_blocks, new_len};

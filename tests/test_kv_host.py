@@ -80,3 +80,14 @@ def test_no_workspace_for_sizes_that_a_call_refuses():
 
     assert size(65536, 1 << 13, 4) == 0 and size(65536, (1 << 13) - 1, 4) > 0
     assert size(2048, 1 << 20, 2) == 0 and size(1023, 1 << 20, 2) > 0
+
+
+def test_accepted_lengths_go_to_none_of_the_inputs():
+    """Every layer reads the tables and the paths while the new lengths are written."""
+    import ctypes
+    from paper_2609_22098_amd import binding as b
+    c = kv.CacheStruct(0x1000, 1 << 20, 8704 * 2, 2, 10, 64, 2, 128)
+    arrays = [0x1000, 0x2000, 0x3000, 0x4000, 0x5000]  # len, n, table, path_nodes, path_len; never dereferenced
+    length, n, table, nodes, count = arrays
+    for new in arrays:
+        assert kv.lib().ts_kv_accept(ctypes.byref(c), length, n, 1, table, 1, nodes, count, new, None) == b.TS_EINVAL
