@@ -150,7 +150,9 @@ size_t ts_kv_attention_workspace_size(const ts_kv_cache* cache, int32_t R, int32
  *      be NULL): DEVICE float [R][cap][q_heads], log sum_t exp(scale <Q, K_t>).
  *      Rows past n[q] of both are left as they were.  Neither may overlap an
  *      input.
- * Scores, softmax statistics and sums are held in fp32.  With TS_F32 nothing is
+ * Scores, softmax statistics and sums are held in fp32; weights are taken against a
+ * maximum that may lag by 2^12, so values near 2^116 over the number of tokens can
+ * overflow their sum.  With TS_F32 nothing is
  * rounded below that.  With TS_BF16
  *   - a query's elements are held to 2^-18 of its head's largest, and the matrix unit
  *     that multiplies 4-bit keys cuts off what is small beside the largest of eight

@@ -37,10 +37,10 @@
 // few tokens, nothing is cut: a workgroup takes a tile.
 //
 // Bounds.  Tiles of 16 rows: bytes (128 requests of one row over 300 to 16000
-// tokens, 557 MB: 116 us, 4.8 TB/s; 131001 tokens of one: 31 us, 4.6 TB/s).  Tiles of
+// tokens, 557 MB: 118 us, 4.7 TB/s; 131001 tokens of one: 32 us, 4.4 TB/s).  Tiles of
 // 128: matrix and vector issue (prompts of 8000 rows over 2000 to 8000 tokens, 675
-// GFLOP: 630 us and 20 for the join, 1.03 PFLOP/s; 64 trees over 500 to 8000: 171 us
-// and 18).  Few short contexts: round trips (a tree of 65 rows over 5003 tokens: 23 us
+// GFLOP: 630 us, 1.07 PFLOP/s, and 21 for the join, once the clocks have risen: 710
+// in the first twenty calls; 64 trees over 500 to 8000: 169 us and 18).  Few short contexts: round trips (a tree of 65 rows over 5003 tokens: 23 us
 // and 7, of which 8 are steps).
 #pragma once
 

@@ -1,6 +1,7 @@
 // Rows into the 4-bit cache, back out of it, and from place to place
 // (ts_kv_append, ts_kv_read, ts_kv_accept).  Bound by bytes where there are many:
-// 16384 rows of 8 heads of 128 take 16 us in and 16.6 us out (5.3 TB/s); one request's
+// 16384 rows of 8 heads of 128, 85 MB, take 20.6 us in and 18.9 us out (4.1 and 4.5
+// TB/s; 16 and 16.6 us where the last-level cache still holds them); one request's
 // take a launch, 2.8 us.
 #pragma once
 
@@ -122,7 +123,8 @@ __global__ __launch_bounds__(kRowThreads) void kv_read_kernel(KvReadParams p) {
 // rows and then writes it, so that no order among the rows matters (a row's new
 // place may be another's old one).  The path is looked up by a wave, a lane to a
 // node.  Bound by lines of 128 bytes, of which a row's codes use 64 and its scales 4 (64
-// requests, 32 layers, 8 heads: 26 us for 17 MB moved); one request's 8.9 us are
+// requests, 32 layers, 8 heads: 30 us for 17 MB moved, 26 where the last-level cache
+// still holds them); one request's 8.9 us are
 // the path's, the table's and the rows' round trips.
 template <int BYTES>
 struct KvPiece;
