@@ -40,8 +40,9 @@
 // tokens, 557 MB: 118 us, 4.7 TB/s; 131001 tokens of one: 32 us, 4.4 TB/s).  Tiles of
 // 128: matrix and vector issue (prompts of 8000 rows over 2000 to 8000 tokens, 675
 // GFLOP: 630 us, 1.07 PFLOP/s, and 21 for the join, once the clocks have risen: 710
-// in the first twenty calls; 64 trees over 500 to 8000: 169 us and 18).  Few short contexts: round trips (a tree of 65 rows over 5003 tokens: 23 us
-// and 7, of which 8 are steps).
+// in the first twenty calls; 64 trees over 500 to 8000: 169 us and 18).  Few short
+// contexts: round trips (a tree of 65 rows over 5003 tokens: 23 us and 7, of which 8
+// are steps).
 #pragma once
 
 #include "kv_format.hpp"
